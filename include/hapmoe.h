@@ -472,6 +472,135 @@ int32_t hapmoe_best_plan_noalloc(const hapmoe_problem *p, const hapmoe_candidate
                                  const hapmoe_dp_result *d_res, const uint8_t *d_types, int64_t n,
                                  int64_t *d_config_best, hapmoe_plan *h_plan, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Operators of a mixture-of-experts training step: the router, the products
+ * grouped by expert, the sum of a token's expert outputs and the optimizer
+ * step.  Their measured times and counts are inputs of the cost model
+ * (expert_tokens and route_coef, t_ffn, opt_coef).  All pointers are device
+ * memory except the arrays of structs; matrices are row-major.  Calls enqueue
+ * work and return; none synchronises or allocates.  Index arrays that these
+ * calls take back (slot, place, offset, expert) are checked on the device: an
+ * index out of range counts as -1, an offset is clamped to the rows. */
+
+/* Element types.  Arithmetic is fp32 everywhere; a 16-bit output is rounded
+ * once, to nearest even. */
+enum { HAPMOE_F32 = 0, HAPMOE_BF16 = 1, HAPMOE_F16 = 2 };
+
+#define HAPMOE_MAX_EXPERTS 1024  /* experts of a routed layer */
+#define HAPMOE_MAX_TOP_K 32      /* experts a token */
+
+/* Workspace of hapmoe_route. */
+int32_t hapmoe_route_ws_bytes(int64_t tokens, int32_t experts, int32_t top_k, int64_t *bytes);
+
+/* Router: of each token's logits x[experts] (row t at d_logits + t * stride
+ * elements) the top_k largest, ties to the lowest expert, in descending order
+ * into d_expert[t * top_k + j], and d_weight: exp(x - max) over its sum, over
+ * all experts or, if renormalize, over the chosen.  A NaN or -inf logit is an
+ * expert closed to the token; where the largest is +inf those experts share
+ * the weight equally.  A token with d_keep[t] = 0 (d_keep may be NULL) takes no
+ * expert.  Choices left over are expert -1 with weight 0.  d_count[experts]
+ * counts the tokens of every expert (the planner's expert_tokens); rows, one
+ * for each (token, choice) with an expert, are ordered by expert, then by t *
+ * top_k + j: expert e has rows d_offset[e] .. d_offset[e + 1], row i holds
+ * choice d_slot[i] = t * top_k + j, and d_place[t * top_k + j] = i.  Unused
+ * places and the slots from d_offset[experts] on are -1.  tokens * top_k <
+ * 2^31. */
+int32_t hapmoe_route(const void *d_logits, int32_t type, int64_t stride, int64_t tokens, int32_t experts,
+                     int32_t top_k, const uint8_t *d_keep, int32_t renormalize, float *d_weight, int32_t *d_expert,
+                     int32_t *d_count, int32_t *d_offset, int32_t *d_slot, int32_t *d_place, void *d_ws,
+                     int64_t ws_bytes, void *stream);
+
+/* Gradient of hapmoe_route's weights: d_d_logits [tokens][experts] of the
+ * logits' type from d_d_weight [tokens][top_k], with the d_expert and d_weight
+ * that the forward call wrote and the same d_keep and renormalize. */
+int32_t hapmoe_route_backward(const void *d_logits, int32_t type, int64_t stride, int64_t tokens, int32_t experts,
+                              int32_t top_k, const uint8_t *d_keep, int32_t renormalize, const int32_t *d_expert,
+                              const float *d_weight, const float *d_d_weight, void *d_d_logits, void *stream);
+
+/* out[t] = sum_j weight[t][j] y[place[t][j]] for y [rows][hidden]: the outputs
+ * of a token's experts put together, added in the order of j.  d_weight NULL:
+ * weights 1 (with place of hapmoe_route the gradient of the rows' copying). */
+int32_t hapmoe_combine(const void *d_y, int32_t type, int64_t rows, int64_t tokens, int32_t top_k, int64_t hidden,
+                       const int32_t *d_place, const float *d_weight, void *d_out, void *stream);
+
+/* Gradients of hapmoe_combine, rows = tokens * top_k: d_d_y [rows][hidden],
+ * row i = weight[slot[i]] d_out[slot[i] / top_k], 0 where slot[i] is -1, and
+ * d_d_weight[t][j] = <d_out[t], y[place[t][j]]>, 0 where place is -1. */
+int32_t hapmoe_combine_backward(const void *d_d_out, const void *d_y, int32_t type, int64_t tokens, int32_t top_k,
+                                int64_t hidden, const int32_t *d_slot, const int32_t *d_place, const float *d_weight,
+                                void *d_d_y, float *d_d_weight, void *stream);
+
+/* Products grouped by expert.  Expert e has rows offset[e] .. offset[e + 1] of
+ * `rows` rows (offset[0] = 0; any number each, none included) and the matrix
+ * w[e] [outputs][inputs].  type BF16 or F16, products summed in fp32. */
+
+/* y[i] = w[e(i)] x[i]  ([rows][outputs]); with d_slot, x[slot[i] / top_k] in
+ * place of x[i], x having x_rows rows `x_stride` elements apart (slot -1: a row
+ * of zeros).  Rows from offset[experts] on are 0. */
+int32_t hapmoe_expert_matmul(const void *d_x, int64_t x_rows, int64_t x_stride, const void *d_w, int32_t type,
+                             int64_t rows, int32_t experts, int64_t outputs, int64_t inputs, const int32_t *d_offset,
+                             const int32_t *d_slot, int32_t top_k, void *d_y, void *stream);
+
+/* d_x[i] = w[e(i)]^T d_y[i]  ([rows][inputs], one row for each row of d_y, rows
+ * `d_y_stride` elements apart).  Rows from offset[experts] on are 0. */
+int32_t hapmoe_expert_matmul_grad_x(const void *d_d_y, int64_t d_y_stride, const void *d_w, int32_t type,
+                                    int64_t rows, int32_t experts, int64_t outputs, int64_t inputs,
+                                    const int32_t *d_offset, void *d_d_x, void *stream);
+
+/* d_w[e] = sum over the rows i of e of d_y[i] x[i]^T  ([outputs][inputs] of
+ * out_type F32 or `type`), 0 for an expert without rows; x as in
+ * hapmoe_expert_matmul.  The order of the sum is fixed. */
+int32_t hapmoe_expert_matmul_grad_w(const void *d_d_y, int64_t d_y_stride, const void *d_x, int64_t x_rows,
+                                    int64_t x_stride, int32_t type, int64_t rows, int32_t experts, int64_t outputs,
+                                    int64_t inputs, const int32_t *d_offset, const int32_t *d_slot, int32_t top_k,
+                                    int32_t out_type, void *d_d_w, void *stream);
+
+/* One tensor of an AdamW step, n elements.  m and v: fp32, or 8-bit codes with
+ * one power of two for every 256 elements (ceil(n / 256) exponents each). */
+typedef struct hapmoe_adamw_tensor {
+    float *param;        /* fp32 master */
+    const void *grad;
+    void *copy;          /* 16-bit copy of the updated master, or NULL (in all tensors with n > 0, or in none) */
+    void *m, *v;
+    int8_t *m_exp, *v_exp;   /* state_bits = 8 only */
+    int64_t n;
+    float weight_decay;
+    int32_t reserved;    /* 0 */
+} hapmoe_adamw_tensor;   /* 72 bytes */
+
+typedef struct hapmoe_adamw_args {
+    double lr, beta1, beta2, eps;
+    double grad_scale;       /* the gradient is grad * grad_scale */
+    int64_t step;            /* 1 for the first */
+    uint64_t seed;           /* of the roundings, state_bits = 8 only; another for every step */
+    const int32_t *d_skip;   /* device; not NULL and not 0 there: nothing is changed */
+    int32_t grad_type;       /* HAPMOE_* */
+    int32_t copy_type;       /* HAPMOE_BF16 or HAPMOE_F16; ignored without copies */
+    int32_t state_bits;      /* 32 or 8 */
+    int32_t reserved;        /* 0 */
+} hapmoe_adamw_args;
+
+/* AdamW over n_tensors tensors (host arrays of structs, read before the call
+ * returns), in place:
+ *   g = grad_scale grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   param -= lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps) + lr weight_decay param
+ * all in fp32.  With state_bits = 8 the fresh m and v enter the step; then they
+ * are rounded.  An 8-bit m is a sign, 4 exponent bits of bias 7 and 3 of
+ * mantissa (127 of them: NaN), times 2^m_exp with m_exp = floor(log2 max |m|) -
+ * 7 over the block; a v 5 exponent bits of bias 15 and 3 of mantissa (255: NaN),
+ * times 2^v_exp, v_exp = floor(log2 max v) - 15 (the maxima from 2^-119 and
+ * 2^-111 on).  Both round up with the probability of what is cut off, so that
+ * the running means do not drift or stick; a v above 0 stays above 0.  The 16
+ * random bits of each are a fixed function of seed and of the element's index
+ * over all tensors, each counted in whole blocks of 256. */
+int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, int32_t n_tensors, const hapmoe_adamw_args *args,
+                     void *stream);
+
+/* The values that n elements of an 8-bit moment stand for, as fp32 or bf16
+ * (exact in both, but for bf16's subnormals): second = 0 for m, 1 for v. */
+int32_t hapmoe_adamw_moment(const uint8_t *d_code, const int8_t *d_exp, int64_t n, int32_t second, int32_t out_type,
+                            void *d_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -211,6 +211,10 @@ int32_t check_problem(const hapmoe_problem *p)
     return HAPMOE_OK;
 }
 
+}  // namespace
+
+namespace hapmoe {
+
 // The architecture check runs on every device call; its answer per device is
 // cached.  Each slot is an atomic written with the same value by whichever
 // thread gets there first, so concurrent callers on any devices are safe.
@@ -228,6 +232,10 @@ int check_arch()
     if (slot) cache[dev].store(ok ? 1 : 2, std::memory_order_relaxed);
     return ok ? HAPMOE_OK : HAPMOE_E_ARCH;
 }
+
+}  // namespace hapmoe
+
+namespace {
 
 struct ImageLayout {
     int64_t off_is_moe, off_tokens, off_pdense, off_pexp, off_act, off_tdense, off_tffn, total;

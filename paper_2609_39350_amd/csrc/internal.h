@@ -125,6 +125,9 @@ inline DebugLayout debug_layout(int n_types, int n_layers)
     return D;
 }
 
+// HAPMOE_OK on a gfx950 device (cached per device)
+int check_arch();
+
 // Kernel launchers (stream = hipStream_t).
 hipError_t launch_cost_tables(const void *d_image, const hapmoe_candidate *d_cand, int64_t per_config,
                               int n_layers, int n_experts, const TablesLayout &L, int64_t cfg_lo, int64_t n_cfg,
