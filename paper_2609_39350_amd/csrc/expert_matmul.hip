@@ -68,21 +68,38 @@ struct Tile {
     int q, p;     // tile of its rows and of the columns
 };
 
-// Tile `id` of the products whose rows are ragged: expert by expert, the column tiles one after another and for each the
-// expert's row tiles, so that workgroups of neighbouring numbers share a column tile of the weights.  Every wave finds
-// it by itself: 64 experts at a time, a scan over their tiles.  False past the last tile.
+// Workgroup -> tile.  Workgroups go to the eight XCDs in turn; each XCD gets a run of neighbouring tiles, which share
+// rows or columns in its L2.  -1 past the last tile.
+__device__ inline int64_t xcd_order(int64_t block, int64_t tiles)
+{
+    const int64_t run = (tiles + 7) >> 3;
+    const int64_t id = (block & 7) * run + (block >> 3);
+    return (block >> 3) < run && id < tiles ? id : -1;
+}
+
+// The tile of a workgroup where rows are ragged: expert by expert, the column tiles one after another and for each the
+// expert's row tiles, so that neighbouring tiles share a column tile of the weights.  Every wave finds it by itself: 64
+// experts at a time, a sum over their tiles, then a scan.  False past the last tile.
 template <int BQ>
-__device__ inline bool find_tile(const int32_t *offset, int experts, int64_t rows, int p_tiles, int64_t id, Tile &t)
+__device__ inline bool find_tile(const int32_t *offset, int experts, int64_t rows, int p_tiles, int64_t block, Tile &t)
 {
     const int lane = threadIdx.x & 63;
+    auto range = [&](int e) {
+        if (e < experts) return expert_rows(offset, e, rows);
+        if (e == experts) return make_int2(min(max(offset[experts], 0), (int)rows), (int)rows);
+        return make_int2(0, 0);
+    };
+    int tiles = 0;   // at most rows + experts + 1
+    for (int e0 = 0; e0 <= experts; e0 += 64) {
+        const int2 r = range(e0 + lane);
+        tiles += (r.y - r.x + BQ - 1) / BQ;
+    }
+    tiles = wave_reduce(tiles, Sum());
+    const int64_t id = xcd_order(block, (int64_t)tiles * p_tiles);
+    if (id < 0) return false;
     int64_t before = 0;
     for (int e0 = 0; e0 <= experts; e0 += 64) {
-        const int e = e0 + lane;
-        int2 r = make_int2(0, 0);
-        if (e < experts)
-            r = expert_rows(offset, e, rows);
-        else if (e == experts)
-            r = make_int2(min(max(offset[experts], 0), (int)rows), (int)rows);
+        const int2 r = range(e0 + lane);
         const int64_t mine = (int64_t)((r.y - r.x + BQ - 1) / BQ) * p_tiles;
         int64_t sum = mine;
 #pragma unroll
@@ -134,7 +151,10 @@ __device__ inline u32x4 load8(const short *p, int n)
 // the eight places of a row, so 16 rows at one k lie in 16 different places of two rows' 256 bytes.  Across: rows k take
 // turns at the pairs of places, for the transposing read of rows 0-3, 8-11, ... of a 16-element column.
 __device__ inline int along_place(int i, int c) { return i * 8 + (c ^ ((i >> 1) & 7)); }
-__device__ inline int across_place(int k, int c, int places) { return k * places + (c ^ (((k & 3) | ((k >> 1) & 4)) << 1)); }
+__device__ inline int across_place(int k, int c, int places)
+{
+    return k * places + (c ^ (((k & 3) | ((k >> 1) & 4)) << 1 & (places - 1)));
+}
 
 template <bool ALONG>
 struct Stage {
@@ -214,7 +234,8 @@ __global__ __launch_bounds__(kThreads) void k_product_any(const ExpertProduct a,
     int64_t q_end, p_end, k_end;
     int64_t out_row;
     if constexpr (KIND == kGradW) {
-        const int64_t id = blockIdx.x;
+        const int64_t id = xcd_order(blockIdx.x, (int64_t)a.experts * p_tiles * q_tiles);
+        if (id < 0) return;
         t.expert = (int)(id / ((int64_t)p_tiles * q_tiles));
         const int local = (int)(id % ((int64_t)p_tiles * q_tiles));
         t.q = local % q_tiles;
@@ -296,30 +317,424 @@ hipError_t product_any(const ExpertProduct &a, hipStream_t s)
 {
     const int64_t p_size = KIND == kForward ? a.outputs : a.inputs;
     const int64_t p_tiles = ceil_div(p_size, kB), q_tiles = ceil_div(a.outputs, kB);
-    const int64_t grid = KIND == kGradW ? a.experts * p_tiles * q_tiles : most_row_tiles(a.rows, a.experts, kB) * p_tiles;
+    const int64_t tiles = KIND == kGradW ? a.experts * p_tiles * q_tiles : most_row_tiles(a.rows, a.experts, kB) * p_tiles;
+    const int64_t grid = ceil_div(tiles, 8) * 8;   // whole rounds of the XCDs
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
     hipLaunchKernelGGL((k_product_any<KIND, T, O>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, (int)p_tiles,
                        (int)q_tiles);
     return hipGetLastError();
 }
 
+// ------------------------------------------------------------------ the kernel for whole vectors
+// Rows and columns that begin on 16 bytes, columns and summands in eights.  The loads go from memory straight into LDS
+// (16 bytes a lane, no registers), 64 summands at a time, while earlier tiles are multiplied.  What does not exist
+// (rows past the expert's, summands past the end) is read from a page of zeros.
+namespace fast {
+
+__device__ u32x4 zeros[16];   // 256 bytes, never written
+
+using Shared = __attribute__((address_space(3))) void;
+
+// n / d for n < 2^31 by a multiplication
+struct Divisor {
+    uint32_t factor;
+    int shift;
+    __device__ int operator()(int n) const { return (int)(((uint64_t)(uint32_t)n * factor) >> shift); }
+};
+Divisor divisor(int d)
+{
+    int bits = 0;
+    while ((int64_t(1) << bits) < d) ++bits;
+    return Divisor{(uint32_t)(((uint64_t(1) << (31 + bits)) + d - 1) / d), 31 + bits};
+}
+
+struct Args {
+    ExpertProduct a;
+    Divisor by_top_k;
+    int p_tiles, q_tiles;
+};
+
+// 16 bytes a lane from `from` to LDS at `to` (the wave's first lane; the others follow), counted by vmcnt alone: the
+// caller waits for it, and the compiler, which would wait for it at the next LDS read, does not see it.  Nothing else
+// here uses m0.
+__device__ inline void load_to_lds(uint64_t from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+
+// All but this wave's last LOADS loads into LDS have landed, its LDS reads are done, and so for every wave.
+template <int LOADS>
+__device__ inline void sync_tiles()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+}
+
+// One operand's tiles: kLoads pieces of 16 bytes for each of THREADS threads.
+// ALONG: SIDE rows of 64 summands.  Across: 64 summands of SIDE columns.
+template <bool ALONG, int SIDE, int THREADS, bool GATHER>
+struct Loader {
+    static constexpr int kLoads = SIDE * 8 / THREADS;
+    static constexpr int kPlaces = ALONG ? 8 : SIDE / 8;      // of a row in LDS
+    static constexpr int kRows = THREADS / kPlaces;           // rows of LDS of one load of all threads
+    static_assert(kLoads >= 1 && kRows % 16 == 0, "the order of the places is the same for every load of a thread");
+    uint64_t at[kLoads];    // the next pieces; gathered across: the thread's column in row 0
+    uint32_t step[kLoads];  // along: bytes to the next tile's, 0 where there is no row
+    int64_t ld2;            // bytes between rows
+    const int32_t *slot;    // gathered across: of the expert's first row
+    int next[kLoads];       // gathered across: the slots of the next tile
+    int first;              // summand of the first piece in the tile
+    int k, k_end, rows;
+
+    // i0: first row (along) or column (across), i_end: those that exist; row0: added to the row (along) or summand
+    __device__ void begin(const void *memory, int64_t ld, const int32_t *slots, Divisor by, int64_t row0,
+                          int64_t memory_rows, int64_t i0, int64_t i_end, int summands)
+    {
+        const int tid = threadIdx.x, r = tid / kPlaces;
+        const auto *const bytes = static_cast<const char *>(memory);
+        const uint64_t none = reinterpret_cast<uint64_t>(zeros);
+        k = 0;
+        k_end = summands;
+        ld2 = ld * 2;
+        rows = (int)memory_rows;
+        if constexpr (ALONG) {
+            first = ((tid & 7) ^ ((tid >> 4) & 7)) * 8;
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int64_t i = i0 + j * kRows + r;
+                bool ok = i < i_end;
+                int64_t from = i + row0;
+                if (GATHER && ok) {
+                    const int s = slots[from];
+                    ok = s >= 0;
+                    from = ok ? by(s) : 0;
+                }
+                ok = ok && from < memory_rows;
+                at[j] = ok ? reinterpret_cast<uint64_t>(bytes + from * ld2 + first * 2) : none;
+                step[j] = ok ? 128 : 0;
+            }
+        } else {
+            first = r;
+            const int64_t column = i0 + (across_place(r, tid % kPlaces, kPlaces) - r * kPlaces) * 8;
+            const bool ok = column < i_end;
+            k_end = ok ? summands : 0;
+            if constexpr (GATHER) {
+                at[0] = reinterpret_cast<uint64_t>(bytes + column * 2);
+                slot = slots + row0;
+                fetch();
+            } else {
+#pragma unroll
+                for (int j = 0; j < kLoads; ++j)
+                    at[j] = reinterpret_cast<uint64_t>(bytes + (row0 + j * kRows + r) * ld2 + column * 2);
+            }
+        }
+    }
+    __device__ void fetch()
+    {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int i = k + first + j * kRows;
+            next[j] = i < k_end ? slot[i] : -1;
+        }
+    }
+    // the next tile into LDS at `to`; zeros past the last summand
+    __device__ void issue(uint32_t to, Divisor by)
+    {
+        const uint64_t none = reinterpret_cast<uint64_t>(zeros);
+        const uint32_t mine = to + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+        uint64_t from[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            if constexpr (ALONG) {
+                from[j] = k + first < k_end ? at[j] : none;
+                at[j] += step[j];
+            } else if constexpr (GATHER) {
+                const int r = by(next[j]);
+                from[j] = ((next[j] >= 0) & (r < rows)) ? at[0] + (uint64_t)(r * ld2) : none;
+            } else {
+                from[j] = k + first + j * kRows < k_end ? at[j] : none;
+                at[j] += (uint64_t)(64 * ld2);
+            }
+        }
+        k += 64;
+        if constexpr (!ALONG && GATHER) fetch();
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) load_to_lds(from[j], mine + j * THREADS * 16);
+    }
+};
+
+// A wave's fragments of one half (32 summands) of a tile.
+template <bool ALONG, int N>
+struct Fragments {
+    s16x8 f[N];
+    __device__ void read(const u32x4 *tile, int i0, int k, int lane, int places)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = fragment<ALONG>(tile, i0 + 16 * i, k, lane, places);
+    }
+};
+
+// The rank-th expert by falling number of rows, in classes of a power of two: the long sums begin first and the short
+// ones fill the gaps.  Every wave by itself, 64 experts a lane group.
+__device__ inline int expert_of_rank(const int32_t *offset, int experts, int64_t rows, int rank)
+{
+    constexpr int kGroups = HAPMOE_MAX_EXPERTS / 64;
+    const int lane = threadIdx.x & 63;
+    int size[kGroups], top = -1;   // class of the expert, -1 without rows, -2 past the last
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        size[g] = -2;
+        if (g * 64 >= experts) break;
+        const int e = g * 64 + lane;
+        if (e < experts) {
+            const int2 r = expert_rows(offset, e, rows);
+            size[g] = r.y > r.x ? 31 - __clz(r.y - r.x) : -1;
+        }
+        top = max(top, size[g]);
+    }
+    top = __builtin_amdgcn_readfirstlane(wave_reduce(top, Max()));
+    for (int c = top; c >= -1; --c) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            if (g * 64 >= experts) break;
+            uint64_t in = __ballot(size[g] == c);
+            const int n = __popcll(in);
+            if (rank < n) {
+                for (; rank > 0; --rank) in &= in - 1;
+                return g * 64 + __ffsll((unsigned long long)in) - 1;
+            }
+            rank -= n;
+        }
+    }
+    return 0;   // not reached: rank < experts
+}
+
+// BQ x BP outputs a workgroup of WQ x WP waves.  STAGES tiles of 64 summands in LDS.
+template <int KIND, typename T, typename O, bool GATHER, int BQ, int BP, int WQ, int WP, int STAGES>
+__global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
+{
+    constexpr bool kQAlong = KIND != kGradW, kPAlong = KIND == kForward;
+    constexpr int kThreads = 64 * WQ * WP;
+    constexpr int kTileQ = BQ * 8, kTile = (BQ + BP) * 8;   // of LDS, in 16 bytes
+    constexpr int kFq = BQ / WQ / 16, kFp = BP / WP / 16;    // a wave's fragments
+    constexpr int kQPlaces = BQ / 8, kPPlaces = BP / 8;
+    __shared__ u32x4 lds[STAGES * kTile];
+    const ExpertProduct &a = args.a;
+    Tile t;
+    Loader<kQAlong, BQ, kThreads, GATHER && KIND == kForward> lq;
+    Loader<kPAlong, BP, kThreads, GATHER && KIND == kGradW> lp;
+    int64_t q_end, p_end, out_row;
+    int k_end;
+    if constexpr (KIND == kGradW) {
+        const int tiles = args.p_tiles * args.q_tiles, rounds = (tiles + 7) & ~7;
+        const int id = (int)xcd_order(blockIdx.x % rounds, tiles);
+        if (id < 0) return;
+        t.expert = expert_of_rank(a.offset, a.experts, a.rows, blockIdx.x / rounds);
+        t.q = id % args.q_tiles;
+        t.p = id / args.q_tiles;
+        const int2 r = expert_rows(a.offset, t.expert, a.rows);
+        q_end = a.outputs;
+        p_end = a.inputs;
+        k_end = r.y - r.x;
+        out_row = (int64_t)t.expert * a.outputs;
+        lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, r.x, a.rows, (int64_t)t.q * BQ, q_end, k_end);
+        lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, r.x, a.x_rows, (int64_t)t.p * BP, p_end, k_end);
+    } else {
+        if (!find_tile<BQ>(a.offset, a.experts, a.rows, args.p_tiles, blockIdx.x, t)) return;
+        const bool some = t.expert < a.experts;
+        q_end = t.hi - t.lo;
+        p_end = KIND == kForward ? a.outputs : a.inputs;
+        k_end = !some ? 0 : KIND == kForward ? (int)a.inputs : (int)a.outputs;
+        out_row = t.lo;
+        const char *w = static_cast<const char *>(a.w) + (some ? t.expert : 0) * a.outputs * a.inputs * 2;
+        lq.begin(KIND == kForward ? a.x : a.d_y, KIND == kForward ? a.x_stride : a.d_y_stride, a.slot, args.by_top_k,
+                 t.lo, KIND == kForward ? a.x_rows : a.rows, (int64_t)t.q * BQ, some ? q_end : 0, k_end);
+        lp.begin(w, a.inputs, nullptr, args.by_top_k, 0, a.outputs, (int64_t)t.p * BP, p_end, k_end);
+    }
+    constexpr int kLoads = decltype(lq)::kLoads + decltype(lp)::kLoads;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wq = (wave / WP) * (BQ / WQ), wp = (wave % WP) * (BP / WP);
+    f32x4 acc[kFq][kFp] = {};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(Shared *)lds;
+    auto issue = [&](int stage) {
+        lq.issue(lds0 + stage * kTile * 16, args.by_top_k);
+        lp.issue(lds0 + (stage * kTile + kTileQ) * 16, args.by_top_k);
+    };
+    auto multiply = [&](const Fragments<kQAlong, kFq> &fq, const Fragments<kPAlong, kFp> &fp) {
+#pragma unroll
+        for (int i = 0; i < kFq; ++i)
+#pragma unroll
+            for (int j = 0; j < kFp; ++j) acc[i][j] = mfma(fp.f[j], fq.f[i], acc[i][j], T());
+    };
+    if constexpr (STAGES == 2) {
+        // Bound by the products.  Those of one half of a tile hide the LDS reads of the next half, and the loads of a
+        // tile have the time of a whole one: once every wave has read a tile's second half, its LDS takes the tile
+        // after the next.
+        Fragments<kQAlong, kFq> q0f, q1f;
+        Fragments<kPAlong, kFp> p0f, p1f;
+        // a read of LDS, a few products, and so on
+        auto interleave = [] {
+            constexpr int kReads = kFq * (kQAlong ? 1 : 2) + kFp * (kPAlong ? 1 : 2), kProducts = kFq * kFp;
+            constexpr int kEach = kProducts / kReads > 0 ? kProducts / kReads : 1;
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+            }
+            if constexpr (kProducts > kReads * kEach)
+                __builtin_amdgcn_sched_group_barrier(0x008, kProducts - kReads * kEach, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (k_end > 0) {
+            issue(0);
+            issue(1);
+            sync_tiles<kLoads>();
+            p0f.read(lds + kTileQ, wp, 0, lane, kPPlaces);
+            q0f.read(lds, wq, 0, lane, kQPlaces);
+        }
+        int turn = 0;
+        for (int k0 = 0; k0 < k_end; k0 += 64) {
+            const u32x4 *const tile = lds + turn * kTile, *const other = lds + (turn ^ 1) * kTile;
+            p1f.read(tile + kTileQ, wp, 32, lane, kPPlaces);
+            q1f.read(tile, wq, 32, lane, kQPlaces);
+            multiply(q0f, p0f);
+            interleave();
+            sync_tiles<0>();
+            issue(turn);
+            __builtin_amdgcn_sched_barrier(0);
+            p0f.read(other + kTileQ, wp, 0, lane, kPPlaces);
+            q0f.read(other, wq, 0, lane, kQPlaces);
+            multiply(q1f, p1f);
+            interleave();
+            turn ^= 1;
+        }
+    } else {
+        // Bound by the loads of w: all tiles but one are under way.
+        if (k_end > 0)
+            for (int i = 0; i < STAGES - 1; ++i) issue(i);
+        int stage = 0;
+        for (int k0 = 0; k0 < k_end; k0 += 64) {
+            sync_tiles<(STAGES - 2) * kLoads>();
+            issue(stage == 0 ? STAGES - 1 : stage - 1);
+            const u32x4 *const tile = lds + stage * kTile;
+            stage = stage == STAGES - 1 ? 0 : stage + 1;
+#pragma unroll
+            for (int k = 0; k < 64; k += 32) {
+                Fragments<kQAlong, kFq> fq;
+                Fragments<kPAlong, kFp> fp;
+                fp.read(tile + kTileQ, wp, k, lane, kPPlaces);
+                fq.read(tile, wq, k, lane, kQPlaces);
+                multiply(fq, fp);
+            }
+        }
+    }
+    // The last tiles' loads, of zeros, have landed and LDS is read: it takes the results, as many rows at a time as fit,
+    // and they leave it as whole rows of the tile.  A row's places are turned by its number, so that neither the 16 rows
+    // of a write nor a row's read meet in a bank.
+    constexpr int kOut = 16 / (int)sizeof(O);                 // results in 16 bytes
+    constexpr int kRow = BP / kOut;                           // places of a row
+    constexpr int kRounds = BQ * kRow <= STAGES * kTile ? 1 : 2;
+    constexpr int kPart = kFq / kRounds * 16;                 // a wave's rows of a round
+    static_assert(BQ / kRounds * kRow <= STAGES * kTile && kFq % kRounds == 0, "the results' LDS");
+    O *const out = static_cast<O *>(a.out);
+    char *const bytes = reinterpret_cast<char *>(lds);
+#pragma unroll
+    for (int h = 0; h < kRounds; ++h) {
+        sync_tiles<0>();
+#pragma unroll
+        for (int i = 0; i < kPart / 16; ++i) {
+            const int r = wave / WP * kPart + 16 * i + (lane & 15);
+#pragma unroll
+            for (int j = 0; j < kFp; ++j) {
+                const int c = wp + 16 * j + (lane >> 4) * 4;
+                struct alignas(4 * sizeof(O)) Four {
+                    O v[4];
+                } f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f.v[k] = from_f32<O>(acc[h * (kPart / 16) + i][j][k]);
+                *reinterpret_cast<Four *>(bytes + (r * kRow + (c / kOut ^ (r & (kRow - 1)))) * 16 +
+                                          c % kOut * (int)sizeof(O)) = f;
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll 4
+        for (int u = threadIdx.x; u < BQ / kRounds * kRow; u += kThreads) {
+            const int r = u / kRow, c = u % kRow;
+            const int64_t q = (int64_t)t.q * BQ + r / kPart * (BQ / WQ) + h * kPart + r % kPart;
+            const int64_t p = (int64_t)t.p * BP + c * kOut;
+            if (q < q_end && p < p_end)
+                *reinterpret_cast<u32x4 *>(out + (out_row + q) * p_end + p) = lds[r * kRow + (c ^ (r & (kRow - 1)))];
+        }
+    }
+}
+
+template <int KIND, typename T, typename O, int BQ, int BP, int WQ, int WP, int STAGES>
+hipError_t launch(const ExpertProduct &a, hipStream_t s)
+{
+    Args args;
+    args.a = a;
+    args.by_top_k = divisor(a.slot ? a.top_k : 1);
+    args.p_tiles = (int)ceil_div(KIND == kForward ? a.outputs : a.inputs, BP);
+    args.q_tiles = (int)ceil_div(a.outputs, BQ);
+    const int64_t tiles = KIND == kGradW ? a.experts * (ceil_div((int64_t)args.p_tiles * args.q_tiles, 8) * 8)
+                                         : most_row_tiles(a.rows, a.experts, BQ) * args.p_tiles;
+    const int64_t grid = ceil_div(tiles, 8) * 8;
+    if (grid > 0x7fffffff || (int64_t)args.p_tiles * args.q_tiles > 0x7ffffff0) return hipErrorInvalidValue;
+    constexpr int kThreads = 64 * WQ * WP;
+    if (a.slot && KIND != kGradX)
+        hipLaunchKernelGGL((k_product<KIND, T, O, true, BQ, BP, WQ, WP, STAGES>), dim3((unsigned)grid), dim3(kThreads),
+                           0, s, args);
+    else
+        hipLaunchKernelGGL((k_product<KIND, T, O, false, BQ, BP, WQ, WP, STAGES>), dim3((unsigned)grid),
+                           dim3(kThreads), 0, s, args);
+    return hipGetLastError();
+}
+
+template <int KIND, typename T, typename O>
+hipError_t product(const ExpertProduct &a, hipStream_t s)
+{
+    const int64_t some = a.rows / a.experts;   // rows an expert
+    if constexpr (KIND == kGradW) {
+        if (some < 256) return launch<KIND, T, O, 128, 128, 2, 2, 2>(a, s);
+        return launch<KIND, T, O, 256, 256, 2, 4, 2>(a, s);
+    } else {
+        if (some < 32) return launch<KIND, T, O, 32, 128, 1, 4, 4>(a, s);
+        if (some < 128) return launch<KIND, T, O, 128, 256, 2, 4, 2>(a, s);
+        return launch<KIND, T, O, 256, 256, 2, 4, 2>(a, s);
+    }
+}
+
+}  // namespace fast
+
+// whether whole vectors can be loaded and stored
+bool whole_vectors(const ExpertProduct &a)
+{
+    return a.outputs % 8 == 0 && a.inputs % 8 == 0 && a.x_stride % 8 == 0 && a.d_y_stride % 8 == 0 &&
+           aligned(a.x, 16) && aligned(a.w, 16) && aligned(a.d_y, 16) && aligned(a.out, 16);
+}
+
+template <int KIND, typename T, typename O>
+hipError_t product(const ExpertProduct &a, hipStream_t s)
+{
+    return whole_vectors(a) ? fast::product<KIND, T, O>(a, s) : product_any<KIND, T, O>(a, s);
+}
+
 }  // namespace
 
 hipError_t launch_expert_matmul(const ExpertProduct &a, hipStream_t s)
 {
-    return a.type == HAPMOE_BF16 ? product_any<kForward, bf16, bf16>(a, s) : product_any<kForward, f16, f16>(a, s);
+    return a.type == HAPMOE_BF16 ? product<kForward, bf16, bf16>(a, s) : product<kForward, f16, f16>(a, s);
 }
 
 hipError_t launch_expert_matmul_grad_x(const ExpertProduct &a, hipStream_t s)
 {
-    return a.type == HAPMOE_BF16 ? product_any<kGradX, bf16, bf16>(a, s) : product_any<kGradX, f16, f16>(a, s);
+    return a.type == HAPMOE_BF16 ? product<kGradX, bf16, bf16>(a, s) : product<kGradX, f16, f16>(a, s);
 }
 
 hipError_t launch_expert_matmul_grad_w(const ExpertProduct &a, hipStream_t s)
 {
     if (a.type == HAPMOE_BF16)
-        return a.out_type == HAPMOE_F32 ? product_any<kGradW, bf16, float>(a, s) : product_any<kGradW, bf16, bf16>(a, s);
-    return a.out_type == HAPMOE_F32 ? product_any<kGradW, f16, float>(a, s) : product_any<kGradW, f16, f16>(a, s);
+        return a.out_type == HAPMOE_F32 ? product<kGradW, bf16, float>(a, s) : product<kGradW, bf16, bf16>(a, s);
+    return a.out_type == HAPMOE_F32 ? product<kGradW, f16, float>(a, s) : product<kGradW, f16, f16>(a, s);
 }
 
 }  // namespace hapmoe
