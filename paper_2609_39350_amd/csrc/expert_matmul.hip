@@ -10,6 +10,8 @@
 // are neighbours in an output row and are stored at once.  An operand whose
 // memory runs along k is read from LDS 16 bytes a lane, one whose memory runs
 // across k by the transposing LDS read, 4 x 16 elements a row of lanes.
+#include <type_traits>
+
 #include "operators.h"
 
 namespace hapmoe {
@@ -94,26 +96,26 @@ __device__ inline bool find_tile(const int32_t *offset, int experts, int64_t row
         const int2 r = range(e0 + lane);
         tiles += (r.y - r.x + BQ - 1) / BQ;
     }
-    tiles = wave_reduce(tiles, Sum());
+    tiles = __builtin_amdgcn_readfirstlane(wave_reduce(tiles, Sum()));
     const int64_t id = xcd_order(block, (int64_t)tiles * p_tiles);
     if (id < 0) return false;
     int64_t before = 0;
     for (int e0 = 0; e0 <= experts; e0 += 64) {
         const int2 r = range(e0 + lane);
-        const int64_t mine = (int64_t)((r.y - r.x + BQ - 1) / BQ) * p_tiles;
-        int64_t sum = mine;
+        const int mine = (r.y - r.x + BQ - 1) / BQ;
+        int sum = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int64_t o = __shfl_up(sum, d, 64);
+            const int o = __shfl_up(sum, d, 64);
             if (lane >= d) sum += o;
         }
-        const uint64_t has = __ballot(before + sum > id);
+        const uint64_t has = __ballot((before + sum) * p_tiles > id);
         if (has) {
             const int l = __ffsll((unsigned long long)has) - 1;
             const int lo = __builtin_amdgcn_readlane(r.x, l), hi = __builtin_amdgcn_readlane(r.y, l);
-            const int64_t start = before + __shfl(sum - mine, l, 64);
+            const int64_t start = (before + __builtin_amdgcn_readlane(sum - mine, l)) * p_tiles;
             const int q_tiles = (hi - lo + BQ - 1) / BQ;
-            const int local = __builtin_amdgcn_readfirstlane((int)(id - start));
+            const int local = (int)(id - start);
             t.expert = e0 + l;
             t.lo = lo;
             t.hi = hi;
@@ -121,7 +123,7 @@ __device__ inline bool find_tile(const int32_t *offset, int experts, int64_t row
             t.p = local / q_tiles;
             return true;
         }
-        before += __shfl(sum, 63, 64);
+        before += __builtin_amdgcn_readlane(sum, 63);
     }
     return false;
 }
@@ -354,12 +356,31 @@ struct Args {
     int p_tiles, q_tiles;
 };
 
-// 16 bytes a lane from `from` to LDS at `to` (the wave's first lane; the others follow), counted by vmcnt alone: the
+// An address that is the same in all lanes, in scalar registers
+__device__ inline const char *scalar(const char *p)
+{
+    const uint64_t x = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return reinterpret_cast<const char *>((uint64_t)hi << 32 | lo);
+}
+
+// 16 bytes a lane from memory to LDS at `to` (the wave's first lane; the others follow), counted by vmcnt alone: the
 // caller waits for it, and the compiler, which would wait for it at the next LDS read, does not see it.  Nothing else
 // here uses m0.
 __device__ inline void load_to_lds(uint64_t from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ inline void load_to_lds(const char *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(scalar(base)), "s"(to)
+                 : "memory");
+}
+// 4 bytes of each lane's line, for the cache's sake alone: they go to LDS that nobody reads
+__device__ inline void touch(const char *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(scalar(base)), "s"(to)
+                 : "memory");
 }
 
 // All but this wave's last LOADS loads into LDS have landed, its LDS reads are done, and so for every wave.
@@ -371,60 +392,68 @@ __device__ inline void sync_tiles()
 
 // One operand's tiles: kLoads pieces of 16 bytes for each of THREADS threads.
 // ALONG: SIDE rows of 64 summands.  Across: 64 summands of SIDE columns.
+// Rows and columns past the last are read as the last, their results go nowhere; summands past the last are read as
+// others of the row (the last tile's caller clears them).  Gathered rows have addresses of their own, and one that does
+// not exist is read from the zeros; the others are 32-bit offsets from the tile's base, which moves on.
 template <bool ALONG, int SIDE, int THREADS, bool GATHER>
 struct Loader {
     static constexpr int kLoads = SIDE * 8 / THREADS;
     static constexpr int kPlaces = ALONG ? 8 : SIDE / 8;      // of a row in LDS
     static constexpr int kRows = THREADS / kPlaces;           // rows of LDS of one load of all threads
     static_assert(kLoads >= 1 && kRows % 16 == 0, "the order of the places is the same for every load of a thread");
-    uint64_t at[kLoads];    // the next pieces; gathered across: the thread's column in row 0
-    uint32_t step[kLoads];  // along: bytes to the next tile's, 0 where there is no row
+    const char *base;       // of the next tile
+    uint32_t off[kLoads];   // of the pieces
+    int64_t move;           // bytes from a tile to the next
+    uint64_t at[kLoads];    // gathered along: the pieces of the next tile; across: the thread's column of row 0
+    uint32_t step[kLoads];  // gathered along: bytes to the next tile's, 0 where there is no row
     int64_t ld2;            // bytes between rows
     const int32_t *slot;    // gathered across: of the expert's first row
     int next[kLoads];       // gathered across: the slots of the next tile
     int first;              // summand of the first piece in the tile
     int k, k_end, rows;
 
-    // i0: first row (along) or column (across), i_end: those that exist; row0: added to the row (along) or summand
+    // i0: first row (along) or column (across), i_end: those that exist, at least one beyond i0; row0: added to the row
+    // (along) or summand
     __device__ void begin(const void *memory, int64_t ld, const int32_t *slots, Divisor by, int64_t row0,
                           int64_t memory_rows, int64_t i0, int64_t i_end, int summands)
     {
         const int tid = threadIdx.x, r = tid / kPlaces;
         const auto *const bytes = static_cast<const char *>(memory);
-        const uint64_t none = reinterpret_cast<uint64_t>(zeros);
         k = 0;
         k_end = summands;
         ld2 = ld * 2;
         rows = (int)memory_rows;
+        const int left = (int)min((int64_t)SIDE, i_end - i0);   // rows or columns of the tile that exist
         if constexpr (ALONG) {
             first = ((tid & 7) ^ ((tid >> 4) & 7)) * 8;
+            move = 128;
+            base = scalar(bytes + (row0 + i0) * ld2);
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
-                const int64_t i = i0 + j * kRows + r;
-                bool ok = i < i_end;
-                int64_t from = i + row0;
-                if (GATHER && ok) {
-                    const int s = slots[from];
-                    ok = s >= 0;
-                    from = ok ? by(s) : 0;
+                const int i = min(j * kRows + r, left - 1);
+                if constexpr (GATHER) {
+                    const int s = slots[row0 + i0 + i], from = by(s);
+                    const bool ok = s >= 0 && from < rows;
+                    at[j] = ok ? reinterpret_cast<uint64_t>(bytes + from * ld2 + first * 2)
+                               : reinterpret_cast<uint64_t>(zeros);
+                    step[j] = ok ? 128 : 0;
+                } else {
+                    off[j] = (uint32_t)(i * ld2) + first * 2;
                 }
-                ok = ok && from < memory_rows;
-                at[j] = ok ? reinterpret_cast<uint64_t>(bytes + from * ld2 + first * 2) : none;
-                step[j] = ok ? 128 : 0;
             }
         } else {
             first = r;
-            const int64_t column = i0 + (across_place(r, tid % kPlaces, kPlaces) - r * kPlaces) * 8;
-            const bool ok = column < i_end;
-            k_end = ok ? summands : 0;
+            move = 64 * ld2;
+            const int place = across_place(r, tid % kPlaces, kPlaces) - r * kPlaces;
+            const int column = min(place * 8, left - 8);
+            base = scalar(bytes + row0 * ld2 + i0 * 2);
             if constexpr (GATHER) {
-                at[0] = reinterpret_cast<uint64_t>(bytes + column * 2);
+                at[0] = reinterpret_cast<uint64_t>(bytes + (i0 + column) * 2);
                 slot = slots + row0;
                 fetch();
             } else {
 #pragma unroll
-                for (int j = 0; j < kLoads; ++j)
-                    at[j] = reinterpret_cast<uint64_t>(bytes + (row0 + j * kRows + r) * ld2 + column * 2);
+                for (int j = 0; j < kLoads; ++j) off[j] = (uint32_t)((j * kRows + r) * ld2) + column * 2;
             }
         }
     }
@@ -436,29 +465,40 @@ struct Loader {
             next[j] = i < k_end ? slot[i] : -1;
         }
     }
-    // the next tile into LDS at `to`; zeros past the last summand
-    __device__ void issue(uint32_t to, Divisor by)
+    // Piece j of the next tile into LDS at `to`.  TAIL: the tile may end early.
+    template <bool TAIL>
+    __device__ void issue(int j, uint32_t to, Divisor by)
     {
-        const uint64_t none = reinterpret_cast<uint64_t>(zeros);
-        const uint32_t mine = to + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
-        uint64_t from[kLoads];
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            if constexpr (ALONG) {
-                from[j] = k + first < k_end ? at[j] : none;
-                at[j] += step[j];
-            } else if constexpr (GATHER) {
-                const int r = by(next[j]);
-                from[j] = ((next[j] >= 0) & (r < rows)) ? at[0] + (uint64_t)(r * ld2) : none;
-            } else {
-                from[j] = k + first + j * kRows < k_end ? at[j] : none;
-                at[j] += (uint64_t)(64 * ld2);
-            }
+        to += (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024 + j * THREADS * 16;
+        if constexpr (GATHER && ALONG) {
+            load_to_lds(TAIL && k + first >= k_end ? reinterpret_cast<uint64_t>(zeros) : at[j], to);
+            at[j] += step[j];
+        } else if constexpr (GATHER) {
+            const int r = by(next[j]);
+            load_to_lds(((next[j] >= 0) & (r < rows)) ? at[0] + (uint64_t)(r * ld2) : reinterpret_cast<uint64_t>(zeros),
+                        to);
+        } else if constexpr (TAIL) {
+            const int mine = ALONG ? first : first + j * kRows;
+            const int other = ALONG ? 0 : k_end - 1 - k;   // a summand of the tile that exists
+            const uint32_t unit = ALONG ? 2 : (uint32_t)ld2;
+            load_to_lds(base, k + mine < k_end ? off[j] : off[j] - (mine - other) * unit, to);
+        } else {
+            load_to_lds(base, off[j], to);
         }
+    }
+    __device__ void advance()
+    {
         k += 64;
+        base += move;
         if constexpr (!ALONG && GATHER) fetch();
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) load_to_lds(from[j], mine + j * THREADS * 16);
+    }
+    // Zeros for the summands past `left` of the tile in LDS.
+    __device__ static void clear(u32x4 *tile, int left)
+    {
+        for (int u = threadIdx.x; u < SIDE * 8; u += THREADS) {
+            const int k = ALONG ? ((u & 7) ^ (u >> 4 & 7)) * 8 : u / kPlaces;
+            if (k >= left) tile[u] = u32x4{0, 0, 0, 0};
+        }
     }
 };
 
@@ -534,36 +574,53 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
         const int2 r = expert_rows(a.offset, t.expert, a.rows);
         q_end = a.outputs;
         p_end = a.inputs;
-        k_end = r.y - r.x;
+        k_end = __builtin_amdgcn_readfirstlane(r.y - r.x);
+        const int lo = __builtin_amdgcn_readfirstlane(r.x);
         out_row = (int64_t)t.expert * a.outputs;
-        lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, r.x, a.rows, (int64_t)t.q * BQ, q_end, k_end);
-        lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, r.x, a.x_rows, (int64_t)t.p * BP, p_end, k_end);
+        if (k_end > 0) {
+            lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, lo, a.rows, (int64_t)t.q * BQ, q_end, k_end);
+            lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, lo, a.x_rows, (int64_t)t.p * BP, p_end, k_end);
+        }
     } else {
         if (!find_tile<BQ>(a.offset, a.experts, a.rows, args.p_tiles, blockIdx.x, t)) return;
-        const bool some = t.expert < a.experts;
         q_end = t.hi - t.lo;
         p_end = KIND == kForward ? a.outputs : a.inputs;
-        k_end = !some ? 0 : KIND == kForward ? (int)a.inputs : (int)a.outputs;
+        k_end = t.expert == a.experts ? 0 : KIND == kForward ? (int)a.inputs : (int)a.outputs;
         out_row = t.lo;
-        const char *w = static_cast<const char *>(a.w) + (some ? t.expert : 0) * a.outputs * a.inputs * 2;
-        lq.begin(KIND == kForward ? a.x : a.d_y, KIND == kForward ? a.x_stride : a.d_y_stride, a.slot, args.by_top_k,
-                 t.lo, KIND == kForward ? a.x_rows : a.rows, (int64_t)t.q * BQ, some ? q_end : 0, k_end);
-        lp.begin(w, a.inputs, nullptr, args.by_top_k, 0, a.outputs, (int64_t)t.p * BP, p_end, k_end);
+        if (k_end > 0) {
+            const char *w = static_cast<const char *>(a.w) + t.expert * a.outputs * a.inputs * 2;
+            lq.begin(KIND == kForward ? a.x : a.d_y, KIND == kForward ? a.x_stride : a.d_y_stride, a.slot,
+                     args.by_top_k, t.lo, KIND == kForward ? a.x_rows : a.rows, (int64_t)t.q * BQ, q_end, k_end);
+            lp.begin(w, a.inputs, nullptr, args.by_top_k, 0, a.outputs, (int64_t)t.p * BP, p_end, k_end);
+        }
     }
-    constexpr int kLoads = decltype(lq)::kLoads + decltype(lp)::kLoads;
+    constexpr int kLoadsQ = decltype(lq)::kLoads, kLoads = kLoadsQ + decltype(lp)::kLoads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wq = (wave / WP) * (BQ / WQ), wp = (wave % WP) * (BP / WP);
+    const int tiles = (k_end + 63) >> 6, tail = k_end & 63;
     f32x4 acc[kFq][kFp] = {};
     const uint32_t lds0 = (uint32_t)(uintptr_t)(Shared *)lds;
-    auto issue = [&](int stage) {
-        lq.issue(lds0 + stage * kTile * 16, args.by_top_k);
-        lp.issue(lds0 + (stage * kTile + kTileQ) * 16, args.by_top_k);
+    auto issue_one = [&](auto may_end, int j, int stage) {
+        const uint32_t to = lds0 + stage * kTile * 16;
+        if (j < kLoadsQ)
+            lq.template issue<decltype(may_end)::value>(j, to, args.by_top_k);
+        else
+            lp.template issue<decltype(may_end)::value>(j - kLoadsQ, to + kTileQ * 16, args.by_top_k);
     };
-    auto multiply = [&](const Fragments<kQAlong, kFq> &fq, const Fragments<kPAlong, kFp> &fp) {
+    auto issue = [&](int stage) {
 #pragma unroll
-        for (int i = 0; i < kFq; ++i)
+        for (int j = 0; j < kLoads; ++j) issue_one(std::true_type(), j, stage);
+        lq.advance();
+        lp.advance();
+    };
+    auto clear_tail = [&](int stage) {
+        lq.clear(lds + stage * kTile, tail);
+        lp.clear(lds + stage * kTile + kTileQ, tail);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    auto multiply = [&](const Fragments<kQAlong, kFq> &fq, const Fragments<kPAlong, kFp> &fp, int i) {
 #pragma unroll
-            for (int j = 0; j < kFp; ++j) acc[i][j] = mfma(fp.f[j], fq.f[i], acc[i][j], T());
+        for (int j = 0; j < kFp; ++j) acc[i][j] = mfma(fp.f[j], fq.f[i], acc[i][j], T());
     };
     if constexpr (STAGES == 2) {
         // Bound by the products.  Those of one half of a tile hide the LDS reads of the next half, and the loads of a
@@ -571,50 +628,72 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
         // after the next.
         Fragments<kQAlong, kFq> q0f, q1f;
         Fragments<kPAlong, kFp> p0f, p1f;
-        // a read of LDS, a few products, and so on
-        auto interleave = [] {
-            constexpr int kReads = kFq * (kQAlong ? 1 : 2) + kFp * (kPAlong ? 1 : 2), kProducts = kFq * kFp;
-            constexpr int kEach = kProducts / kReads > 0 ? kProducts / kReads : 1;
+        // the products of one half with the reads of the next among them, and with the loads of a tile (ISSUE 1; 2: it
+        // may end early) among both
+        auto half = [&](auto issue_mode, int into, const u32x4 *tile, int k, const Fragments<kQAlong, kFq> &fq,
+                        const Fragments<kPAlong, kFp> &fp, Fragments<kQAlong, kFq> &nq, Fragments<kPAlong, kFp> &np) {
+            constexpr int kMode = decltype(issue_mode)::value;
+            constexpr int kReads = kFq + kFp;
 #pragma unroll
-            for (int i = 0; i < kReads; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+            for (int i = 0; i < kFq; ++i) {
+                if constexpr (kMode > 0) {
+#pragma unroll
+                    for (int j = i * kLoads / kFq; j < (i + 1) * kLoads / kFq; ++j)
+                        issue_one(std::integral_constant<bool, kMode == 2>(), j, into);
+                }
+#pragma unroll
+                for (int r = i * kReads / kFq; r < (i + 1) * kReads / kFq; ++r) {
+                    if (r < kFp)
+                        np.f[r] = fragment<kPAlong>(tile + kTileQ, wp + 16 * r, k, lane, kPPlaces);
+                    else
+                        nq.f[r - kFp] = fragment<kQAlong>(tile, wq + 16 * (r - kFp), k, lane, kQPlaces);
+                }
+                multiply(fq, fp, i);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if constexpr (kProducts > kReads * kEach)
-                __builtin_amdgcn_sched_group_barrier(0x008, kProducts - kReads * kEach, 0);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kMode > 0) {
+                lq.advance();
+                lp.advance();
+            }
         };
-        if (k_end > 0) {
+        int turn = 0;
+        auto step = [&](auto issue_mode, bool last_is_next) {
+            half(std::integral_constant<int, 0>(), 0, lds + turn * kTile, 32, q0f, p0f, q1f, p1f);
+            sync_tiles<0>();
+            if (last_is_next) clear_tail(turn ^ 1);
+            half(issue_mode, turn, lds + (turn ^ 1) * kTile, 0, q1f, p1f, q0f, p0f);
+            turn ^= 1;
+        };
+        if (tiles > 0) {
             issue(0);
-            issue(1);
-            sync_tiles<kLoads>();
+            if (tiles > 1) {
+                issue(1);
+                sync_tiles<kLoads>();
+            } else {
+                sync_tiles<0>();
+                if (tail) clear_tail(0);
+            }
             p0f.read(lds + kTileQ, wp, 0, lane, kPPlaces);
             q0f.read(lds, wq, 0, lane, kQPlaces);
         }
-        int turn = 0;
-        for (int k0 = 0; k0 < k_end; k0 += 64) {
-            const u32x4 *const tile = lds + turn * kTile, *const other = lds + (turn ^ 1) * kTile;
-            p1f.read(tile + kTileQ, wp, 32, lane, kPPlaces);
-            q1f.read(tile, wq, 32, lane, kQPlaces);
-            multiply(q0f, p0f);
-            interleave();
-            sync_tiles<0>();
-            issue(turn);
-            __builtin_amdgcn_sched_barrier(0);
-            p0f.read(other + kTileQ, wp, 0, lane, kPPlaces);
-            q0f.read(other, wq, 0, lane, kQPlaces);
-            multiply(q1f, p1f);
-            interleave();
-            turn ^= 1;
+        int i = 0;
+        for (; i + 3 < tiles; ++i) step(std::integral_constant<int, 1>(), false);
+        if (i + 2 < tiles) {
+            step(std::integral_constant<int, 2>(), false);
+            ++i;
         }
+        for (; i < tiles; ++i) step(std::integral_constant<int, 0>(), tail != 0 && i + 2 == tiles);
     } else {
         // Bound by the loads of w: all tiles but one are under way.
-        if (k_end > 0)
-            for (int i = 0; i < STAGES - 1; ++i) issue(i);
+        for (int i = 0; i < STAGES - 1 && i < tiles; ++i) issue(i);
         int stage = 0;
-        for (int k0 = 0; k0 < k_end; k0 += 64) {
-            sync_tiles<(STAGES - 2) * kLoads>();
-            issue(stage == 0 ? STAGES - 1 : stage - 1);
+        for (int i = 0; i < tiles; ++i) {
+            if (i + STAGES - 1 < tiles + 1)
+                sync_tiles<(STAGES - 2) * kLoads>();
+            else
+                sync_tiles<0>();
+            if (i + STAGES - 1 < tiles) issue(stage == 0 ? STAGES - 1 : stage - 1);
+            if (tail && i + 1 == tiles) clear_tail(stage);
             const u32x4 *const tile = lds + stage * kTile;
             stage = stage == STAGES - 1 ? 0 : stage + 1;
 #pragma unroll
@@ -623,12 +702,12 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
                 Fragments<kPAlong, kFp> fp;
                 fp.read(tile + kTileQ, wp, k, lane, kPPlaces);
                 fq.read(tile, wq, k, lane, kQPlaces);
-                multiply(fq, fp);
+#pragma unroll
+                for (int f = 0; f < kFq; ++f) multiply(fq, fp, f);
             }
         }
     }
-    // The last tiles' loads, of zeros, have landed and LDS is read: it takes the results, as many rows at a time as fit,
-    // and they leave it as whole rows of the tile.  A row's places are turned by its number, so that neither the 16 rows
+    // LDS is read: it takes the results, as many rows at a time as fit, and they leave it as whole rows of the tile.  A row's places are turned by its number, so that neither the 16 rows
     // of a write nor a row's read meet in a bank.
     constexpr int kOut = 16 / (int)sizeof(O);                 // results in 16 bytes
     constexpr int kRow = BP / kOut;                           // places of a row
@@ -708,7 +787,8 @@ hipError_t product(const ExpertProduct &a, hipStream_t s)
 // whether whole vectors can be loaded and stored
 bool whole_vectors(const ExpertProduct &a)
 {
-    return a.outputs % 8 == 0 && a.inputs % 8 == 0 && a.x_stride % 8 == 0 && a.d_y_stride % 8 == 0 &&
+    constexpr int64_t kFar = int64_t(1) << 22;   // 256 rows this many elements long are within 32-bit offsets
+    return a.inputs <= kFar && a.outputs <= kFar && a.x_stride <= kFar && a.d_y_stride <= kFar && a.outputs % 8 == 0 && a.inputs % 8 == 0 && a.x_stride % 8 == 0 && a.d_y_stride % 8 == 0 &&
            aligned(a.x, 16) && aligned(a.w, 16) && aligned(a.d_y, 16) && aligned(a.out, 16);
 }
 
