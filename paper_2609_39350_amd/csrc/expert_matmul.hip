@@ -391,24 +391,27 @@ __device__ inline void sync_tiles()
 }
 
 // One operand's tiles: kLoads pieces of 16 bytes for each of THREADS threads.
-// ALONG: SIDE rows of 64 summands.  Across: 64 summands of SIDE columns.
+// ALONG: SIDE rows of DEPTH summands.  Across: DEPTH summands of SIDE columns.
 // Rows and columns past the last are read as the last, their results go nowhere; summands past the last are read as
 // others of the row (the last tile's caller clears them).  Gathered rows have addresses of their own, and one that does
 // not exist is read from the zeros; the others are 32-bit offsets from the tile's base, which moves on.
-template <bool ALONG, int SIDE, int THREADS, bool GATHER>
+template <bool ALONG, int SIDE, int THREADS, bool GATHER, int DEPTH = 64>
 struct Loader {
-    static constexpr int kLoads = SIDE * 8 / THREADS;
+    static constexpr int kLoads = SIDE * DEPTH / 8 / THREADS;
     static constexpr int kPlaces = ALONG ? 8 : SIDE / 8;      // of a row in LDS
     static constexpr int kRows = THREADS / kPlaces;           // rows of LDS of one load of all threads
-    static_assert(kLoads >= 1 && kRows % 16 == 0, "the order of the places is the same for every load of a thread");
+    static_assert(kLoads >= 1 && (ALONG ? DEPTH == 64 && kRows % 16 == 0 : kRows * kLoads == DEPTH), "whole tiles");
     const char *base;       // of the next tile
     uint32_t off[kLoads];   // of the pieces
     int64_t move;           // bytes from a tile to the next
-    uint64_t at[kLoads];    // gathered along: the pieces of the next tile; across: the thread's column of row 0
+    uint64_t at[kLoads];    // gathered along: the pieces of the next tile
     uint32_t step[kLoads];  // gathered along: bytes to the next tile's, 0 where there is no row
     int64_t ld2;            // bytes between rows
-    const int32_t *slot;    // gathered across: of the expert's first row
-    int next[kLoads];       // gathered across: the slots of the next tile
+    // gathered across: a wave's piece is two rows, whose slots are scalars
+    using Slots = __attribute__((address_space(4))) const int32_t;
+    Slots *slot;            // of the expert's first row
+    int next[kLoads][2];    // the slots of the next tile
+    uint32_t column[kLoads];
     int first;              // summand of the first piece in the tile
     int k, k_end, rows;
 
@@ -443,27 +446,33 @@ struct Loader {
             }
         } else {
             first = r;
-            move = 64 * ld2;
-            const int place = across_place(r, tid % kPlaces, kPlaces) - r * kPlaces;
-            const int column = min(place * 8, left - 8);
+            move = DEPTH * ld2;
             base = scalar(bytes + row0 * ld2 + i0 * 2);
-            if constexpr (GATHER) {
-                at[0] = reinterpret_cast<uint64_t>(bytes + (i0 + column) * 2);
-                slot = slots + row0;
-                fetch();
-            } else {
 #pragma unroll
-                for (int j = 0; j < kLoads; ++j) off[j] = (uint32_t)((j * kRows + r) * ld2) + column * 2;
+            for (int j = 0; j < kLoads; ++j) {
+                const int k = j * kRows + r, place = across_place(k, tid % kPlaces, kPlaces) - k * kPlaces;
+                const int column = min(place * 8, left - 8);
+                if constexpr (GATHER)
+                    this->column[j] = column * 2;
+                else
+                    off[j] = (uint32_t)(k * ld2) + column * 2;
+            }
+            if constexpr (GATHER) {
+                static_assert(kPlaces == 32, "two rows a wave");
+                base = scalar(bytes + i0 * 2);
+                slot = (Slots *)(uintptr_t)scalar(reinterpret_cast<const char *>(slots + row0));
+                fetch();
             }
         }
     }
     __device__ void fetch()
     {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int i = k + first + j * kRows;
-            next[j] = i < k_end ? slot[i] : -1;
-        }
+        for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                next[j][h] = slot[min(k + j * kRows + wave * 2 + h, k_end - 1)];
     }
     // Piece j of the next tile into LDS at `to`.  TAIL: the tile may end early.
     template <bool TAIL>
@@ -474,9 +483,20 @@ struct Loader {
             load_to_lds(TAIL && k + first >= k_end ? reinterpret_cast<uint64_t>(zeros) : at[j], to);
             at[j] += step[j];
         } else if constexpr (GATHER) {
-            const int r = by(next[j]);
-            load_to_lds(((next[j] >= 0) & (r < rows)) ? at[0] + (uint64_t)(r * ld2) : reinterpret_cast<uint64_t>(zeros),
-                        to);
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            uint64_t row[2];
+            uint32_t there[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = by(next[j][h]);
+                const bool some = (next[j][h] >= 0) & (r < rows) & (!TAIL | (k + j * kRows + wave * 2 + h < k_end));
+                const uint64_t ok = some ? ~uint64_t(0) : 0;
+                row[h] = (reinterpret_cast<uint64_t>(base) + (uint64_t)(r * ld2)) & ok;
+                row[h] |= reinterpret_cast<uint64_t>(zeros) & ~ok;
+                there[h] = (uint32_t)ok;
+            }
+            const bool low = (threadIdx.x & 32) == 0;
+            load_to_lds((low ? row[0] : row[1]) + (column[j] & (low ? there[0] : there[1])), to);
         } else if constexpr (TAIL) {
             const int mine = ALONG ? first : first + j * kRows;
             const int other = ALONG ? 0 : k_end - 1 - k;   // a summand of the tile that exists
@@ -488,14 +508,16 @@ struct Loader {
     }
     __device__ void advance()
     {
-        k += 64;
-        base += move;
-        if constexpr (!ALONG && GATHER) fetch();
+        k += DEPTH;
+        if constexpr (!ALONG && GATHER)
+            fetch();
+        else
+            base += move;
     }
     // Zeros for the summands past `left` of the tile in LDS.
     __device__ static void clear(u32x4 *tile, int left)
     {
-        for (int u = threadIdx.x; u < SIDE * 8; u += THREADS) {
+        for (int u = threadIdx.x; u < SIDE * DEPTH / 8; u += THREADS) {
             const int k = ALONG ? ((u & 7) ^ (u >> 4 & 7)) * 8 : u / kPlaces;
             if (k >= left) tile[u] = u32x4{0, 0, 0, 0};
         }
@@ -546,6 +568,50 @@ __device__ inline int expert_of_rank(const int32_t *offset, int experts, int64_t
         }
     }
     return 0;   // not reached: rank < experts
+}
+
+// The results of a workgroup's waves to rows q0 .. q_end of out, columns p0 .. p_end.  LDS is read by now: it takes them,
+// as many rows at a time as fit, and they leave it as whole rows of the tile.  A row's places are turned by its number,
+// so that neither the 16 rows of a write nor a row's read meet in a bank.
+template <typename O, int BQ, int BP, int WQ, int WP, int SPACE>
+__device__ inline void store_tile(u32x4 *lds, const f32x4 (&acc)[BQ / WQ / 16][BP / WP / 16], O *out, int64_t q0,
+                                  int64_t q_end, int64_t p0, int64_t p_end)
+{
+    constexpr int kThreads = 64 * WQ * WP, kFq = BQ / WQ / 16, kFp = BP / WP / 16;
+    constexpr int kOut = 16 / (int)sizeof(O);                 // results in 16 bytes
+    constexpr int kRow = BP / kOut;                           // places of a row
+    constexpr int kRounds = BQ * kRow <= SPACE ? 1 : 2;
+    constexpr int kPart = kFq / kRounds * 16;                 // a wave's rows of a round
+    static_assert(BQ / kRounds * kRow <= SPACE && kFq % kRounds == 0, "the results' LDS");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = (wave % WP) * (BP / WP);
+    char *const bytes = reinterpret_cast<char *>(lds);
+#pragma unroll
+    for (int h = 0; h < kRounds; ++h) {
+        sync_tiles<0>();
+#pragma unroll
+        for (int i = 0; i < kPart / 16; ++i) {
+            const int r = wave / WP * kPart + 16 * i + (lane & 15);
+#pragma unroll
+            for (int j = 0; j < kFp; ++j) {
+                const int c = wp + 16 * j + (lane >> 4) * 4;
+                struct alignas(4 * sizeof(O)) Four {
+                    O v[4];
+                } f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f.v[k] = from_f32<O>(acc[h * (kPart / 16) + i][j][k]);
+                *reinterpret_cast<Four *>(bytes + (r * kRow + (c / kOut ^ (r & (kRow - 1)))) * 16 +
+                                          c % kOut * (int)sizeof(O)) = f;
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll 4
+        for (int u = threadIdx.x; u < BQ / kRounds * kRow; u += kThreads) {
+            const int r = u / kRow, c = u % kRow;
+            const int64_t q = q0 + r / kPart * (BQ / WQ) + h * kPart + r % kPart, p = p0 + c * kOut;
+            if (q < q_end && p < p_end)
+                *reinterpret_cast<u32x4 *>(out + q * p_end + p) = lds[r * kRow + (c ^ (r & (kRow - 1)))];
+        }
+    }
 }
 
 // BQ x BP outputs a workgroup of WQ x WP waves.  STAGES tiles of 64 summands in LDS.
@@ -707,43 +773,102 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
             }
         }
     }
-    // LDS is read: it takes the results, as many rows at a time as fit, and they leave it as whole rows of the tile.  A row's places are turned by its number, so that neither the 16 rows
-    // of a write nor a row's read meet in a bank.
-    constexpr int kOut = 16 / (int)sizeof(O);                 // results in 16 bytes
-    constexpr int kRow = BP / kOut;                           // places of a row
-    constexpr int kRounds = BQ * kRow <= STAGES * kTile ? 1 : 2;
-    constexpr int kPart = kFq / kRounds * 16;                 // a wave's rows of a round
-    static_assert(BQ / kRounds * kRow <= STAGES * kTile && kFq % kRounds == 0, "the results' LDS");
-    O *const out = static_cast<O *>(a.out);
-    char *const bytes = reinterpret_cast<char *>(lds);
+    store_tile<O, BQ, BP, WQ, WP, STAGES * kTile>(lds, acc, static_cast<O *>(a.out) + out_row * p_end, (int64_t)t.q * BQ,
+                                                  q_end, (int64_t)t.p * BP, p_end);
+}
+
+// d_w: BQ x BP outputs of one expert a workgroup of four waves, 32 rows at a time, three tiles in LDS, two workgroups a
+// CU: the one's LDS reads and results leave while the other multiplies.  A tile's loads have the time of two.
+template <typename T, typename O, bool GATHER, int BQ, int BP>
+__global__ __launch_bounds__(256, 2) void k_grad_w(const Args args)
+{
+    constexpr int kThreads = 256, kDepth = 32, kStages = 3, kWQ = 2, kWP = 2;
+    constexpr int kTileQ = BQ * kDepth / 8, kTileP = BP * kDepth / 8;   // of LDS, in 16 bytes
+    constexpr int kFq = BQ / kWQ / 16, kFp = BP / kWP / 16;
+    __shared__ u32x4 lds[kStages * (kTileQ + kTileP)];
+    const ExpertProduct &a = args.a;
+    const int per = args.p_tiles * args.q_tiles, rounds = (per + 7) & ~7;
+    const int id = (int)xcd_order(blockIdx.x % rounds, per);
+    if (id < 0) return;
+    const int expert = expert_of_rank(a.offset, a.experts, a.rows, blockIdx.x / rounds);
+    const int64_t q0 = (int64_t)(id % args.q_tiles) * BQ, p0 = (int64_t)(id / args.q_tiles) * BP;
+    const int2 range = expert_rows(a.offset, expert, a.rows);
+    const int lo = __builtin_amdgcn_readfirstlane(range.x), k_end = __builtin_amdgcn_readfirstlane(range.y) - lo;
+    Loader<false, BQ, kThreads, false, kDepth> lq;
+    Loader<false, BP, kThreads, GATHER, kDepth> lp;
+    constexpr int kLoadsQ = decltype(lq)::kLoads, kLoads = kLoadsQ + decltype(lp)::kLoads;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wq = wave / kWP * (BQ / kWQ), wp = wave % kWP * (BP / kWP);
+    const int tiles = (k_end + kDepth - 1) / kDepth, tail = k_end % kDepth;
+    f32x4 acc[kFq][kFp] = {};
+    u32x4 *const lds_q = lds, *const lds_p = lds + kStages * kTileQ;
+    const uint32_t to_q = (uint32_t)(uintptr_t)(Shared *)lds_q, to_p = (uint32_t)(uintptr_t)(Shared *)lds_p;
+    auto issue_one = [&](auto may_end, int j, int stage) {
+        if (j < kLoadsQ)
+            lq.template issue<decltype(may_end)::value>(j, to_q + stage * kTileQ * 16, args.by_top_k);
+        else
+            lp.template issue<decltype(may_end)::value>(j - kLoadsQ, to_p + stage * kTileP * 16, args.by_top_k);
+    };
+    auto issue = [&](int stage) {
 #pragma unroll
-    for (int h = 0; h < kRounds; ++h) {
-        sync_tiles<0>();
-#pragma unroll
-        for (int i = 0; i < kPart / 16; ++i) {
-            const int r = wave / WP * kPart + 16 * i + (lane & 15);
-#pragma unroll
-            for (int j = 0; j < kFp; ++j) {
-                const int c = wp + 16 * j + (lane >> 4) * 4;
-                struct alignas(4 * sizeof(O)) Four {
-                    O v[4];
-                } f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) f.v[k] = from_f32<O>(acc[h * (kPart / 16) + i][j][k]);
-                *reinterpret_cast<Four *>(bytes + (r * kRow + (c / kOut ^ (r & (kRow - 1)))) * 16 +
-                                          c % kOut * (int)sizeof(O)) = f;
-            }
-        }
+        for (int j = 0; j < kLoads; ++j) issue_one(std::true_type(), j, stage);
+        lq.advance();
+        lp.advance();
+    };
+    auto clear_tail = [&](int stage) {
+        lq.clear(lds_q + stage * kTileQ, tail);
+        lp.clear(lds_p + stage * kTileP, tail);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll 4
-        for (int u = threadIdx.x; u < BQ / kRounds * kRow; u += kThreads) {
-            const int r = u / kRow, c = u % kRow;
-            const int64_t q = (int64_t)t.q * BQ + r / kPart * (BQ / WQ) + h * kPart + r % kPart;
-            const int64_t p = (int64_t)t.p * BP + c * kOut;
-            if (q < q_end && p < p_end)
-                *reinterpret_cast<u32x4 *>(out + (out_row + q) * p_end + p) = lds[r * kRow + (c ^ (r & (kRow - 1)))];
-        }
+    };
+    if (tiles > 0) {
+        lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, lo, a.rows, q0, a.outputs, k_end);
+        lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, lo, a.x_rows, p0, a.inputs, k_end);
+        issue(0);
+        if (tiles > 1) issue(1);
     }
+    // mode 0: none left to load, 1: a whole tile, 2: one that may end early
+    auto step = [&](auto mode, int i, int stage) {
+        constexpr int kMode = decltype(mode)::value;
+        if (kMode > 0 || i + 1 < tiles)
+            sync_tiles<kLoads>();
+        else
+            sync_tiles<0>();
+        if (kMode == 0 && tail && i + 1 == tiles) clear_tail(stage);
+        const int into = stage == 0 ? kStages - 1 : stage - 1;
+        const u32x4 *const tq = lds_q + stage * kTileQ, *const tp = lds_p + stage * kTileP;
+        Fragments<false, kFq> fq;
+        Fragments<false, kFp> fp;
+        fp.read(tp, wp, 0, lane, BP / 8);
+        fq.f[0] = fragment<false>(tq, wq, 0, lane, BQ / 8);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < kFq; ++f) {
+            if constexpr (kMode > 0) {
+#pragma unroll
+                for (int j = f * kLoads / kFq; j < (f + 1) * kLoads / kFq; ++j)
+                    issue_one(std::integral_constant<bool, kMode == 2>(), j, into);
+            }
+            if (f + 1 < kFq) fq.f[f + 1] = fragment<false>(tq, wq + 16 * (f + 1), 0, lane, BQ / 8);
+#pragma unroll
+            for (int j = 0; j < kFp; ++j) acc[f][j] = mfma(fp.f[j], fq.f[f], acc[f][j], T());
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (kMode > 0) {
+            lq.advance();
+            lp.advance();
+        }
+    };
+    int i = 0, stage = 0;
+    auto turn = [&] { stage = stage == kStages - 1 ? 0 : stage + 1; };
+    for (; i + 3 < tiles; ++i, turn()) step(std::integral_constant<int, 1>(), i, stage);
+    if (i + 2 < tiles) {
+        step(std::integral_constant<int, 2>(), i, stage);
+        ++i;
+        turn();
+    }
+    for (; i < tiles; ++i, turn()) step(std::integral_constant<int, 0>(), i, stage);
+    store_tile<O, BQ, BP, kWQ, kWP, kStages * (kTileQ + kTileP)>(
+        lds, acc, static_cast<O *>(a.out) + expert * a.outputs * a.inputs, q0, a.outputs, p0, a.inputs);
 }
 
 template <int KIND, typename T, typename O, int BQ, int BP, int WQ, int WP, int STAGES>
@@ -768,12 +893,28 @@ hipError_t launch(const ExpertProduct &a, hipStream_t s)
     return hipGetLastError();
 }
 
+template <typename T, typename O, int BQ, int BP>
+hipError_t launch_grad_w(const ExpertProduct &a, hipStream_t s)
+{
+    Args args;
+    args.a = a;
+    args.by_top_k = divisor(a.slot ? a.top_k : 1);
+    args.p_tiles = (int)ceil_div(a.inputs, BP);
+    args.q_tiles = (int)ceil_div(a.outputs, BQ);
+    const int64_t per = (int64_t)args.p_tiles * args.q_tiles;
+    const int64_t grid = a.experts * (ceil_div(per, 8) * 8);   // whole rounds of the XCDs for each expert
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((a.slot ? k_grad_w<T, O, true, BQ, BP> : k_grad_w<T, O, false, BQ, BP>), dim3((unsigned)grid),
+                       dim3(256), 0, s, args);
+    return hipGetLastError();
+}
+
 template <int KIND, typename T, typename O>
 hipError_t product(const ExpertProduct &a, hipStream_t s)
 {
     const int64_t some = a.rows / a.experts;   // rows an expert
     if constexpr (KIND == kGradW) {
-        if (some < 256) return launch<KIND, T, O, 128, 128, 2, 2, 2>(a, s);
+        if (some < 512) return launch_grad_w<T, O, 128, 256>(a, s);
         return launch<KIND, T, O, 256, 256, 2, 4, 2>(a, s);
     } else {
         if (some < 32) return launch<KIND, T, O, 32, 128, 1, 4, 4>(a, s);
