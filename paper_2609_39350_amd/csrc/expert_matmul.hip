@@ -917,8 +917,8 @@ hipError_t product(const ExpertProduct &a, hipStream_t s)
         if (some < 512) return launch_grad_w<T, O, 128, 256>(a, s);
         return launch<KIND, T, O, 256, 256, 2, 4, 2>(a, s);
     } else {
-        if (some < 32) return launch<KIND, T, O, 32, 128, 1, 4, 4>(a, s);
-        if (some < 128) return launch<KIND, T, O, 128, 256, 2, 4, 2>(a, s);
+        if (some < 48) return launch<KIND, T, O, 64, 128, 2, 2, 3>(a, s);
+        if (some < 192) return launch<KIND, T, O, 128, 128, 2, 2, 2>(a, s);
         return launch<KIND, T, O, 256, 256, 2, 4, 2>(a, s);
     }
 }

@@ -71,8 +71,15 @@ def _check(code, what):
         raise binding.HapmoeError(code, what)
 
 
-def _stream():
-    return torch.cuda.current_stream().cuda_stream
+try:   # the current stream's address without an object for it: 0.1 us of a call, where the object takes 2
+    from torch._C import _cuda_getCurrentRawStream as _stream_of
+except ImportError:
+    def _stream_of(index):
+        return torch.cuda.current_stream(index).cuda_stream
+
+
+def _stream(t):
+    return _stream_of(t.get_device())
 
 
 def _need(ok, what):
@@ -81,31 +88,39 @@ def _need(ok, what):
 
 
 def _on_device(name, t):
-    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name}: a tensor on the GPU")
-    _need(t.device.index == torch.cuda.current_device(), f"{name}: on {t.device}, which is not the current device")
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise ValueError(f"{name}: a tensor on the GPU")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, which is not the current device")
 
 
-def _array(name, t, dtype, shape):
+# The checks below run on every call: their messages are put together only where one is due.
+def _array(name, t, dtype, *shape):
     """A contiguous tensor of this type and shape (None in the shape: any)."""
     _on_device(name, t)
-    _need(t.dtype == dtype, f"{name}: {dtype}, not {t.dtype}")
-    _need(len(t.shape) == len(shape) and all(s is None or a == s for a, s in zip(t.shape, shape)),
-          f"{name}: shape {tuple(shape)}, not {tuple(t.shape)}")
-    _need(t.is_contiguous(), f"{name}: contiguous")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {dtype}, not {t.dtype}")
+    if t.dim() != len(shape) or any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise ValueError(f"{name}: shape {shape}, not {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous")
 
 
 def _matrix(name, t, types):
     """A matrix of one of the types whose rows are contiguous; the distance of its rows in elements."""
     _on_device(name, t)
-    _need(t.dtype in types, f"{name}: one of {', '.join(str(x) for x in types)}, not {t.dtype}")
-    _need(t.dim() == 2, f"{name}: a matrix, not {t.dim()} dimensions")
+    if t.dtype not in types:
+        raise ValueError(f"{name}: one of {', '.join(str(x) for x in types)}, not {t.dtype}")
+    if t.dim() != 2 or t.shape[1] == 0:
+        raise ValueError(f"{name}: a matrix with columns, not {tuple(t.shape)}")
     rows, columns = t.shape
-    _need(columns > 0, f"{name}: no columns")
     step, unit = t.stride()
-    _need(columns == 1 or unit == 1, f"{name}: its rows have to be contiguous")
+    if unit != 1 and columns > 1:
+        raise ValueError(f"{name}: its rows have to be contiguous")
     if rows <= 1:
         return columns
-    _need(step >= columns, f"{name}: its rows overlap")
+    if step < columns:
+        raise ValueError(f"{name}: its rows overlap")
     return step
 
 
@@ -133,13 +148,14 @@ class Routing:
         self.slot = torch.empty(tokens * top_k, **i32)
         self.place = torch.empty((tokens, top_k), **i32)
         self._ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+        self._outputs = tuple(t.data_ptr() for t in (self.weight, self.expert, self.count, self.offset, self.slot,
+                                                     self.place, self._ws)) + (need.value,)
 
 
 def _keep(keep, tokens):
     if keep is None:
         return None
-    _need(keep.dtype in (torch.bool, torch.uint8), f"keep: torch.bool or torch.uint8, not {keep.dtype}")
-    _array("keep", keep, keep.dtype, (tokens,))
+    _array("keep", keep, torch.uint8 if keep.dtype == torch.uint8 else torch.bool, tokens)
     return keep.data_ptr()
 
 
@@ -155,10 +171,8 @@ def route(logits, top_k: int, keep=None, renormalize=True, out: Routing = None) 
         _need((out.tokens, out.experts, out.top_k) == (tokens, experts, top_k) and
               out.expert.device == logits.device, "out: made for other sizes or another device")
     _check(_lib().hapmoe_route(logits.data_ptr(), _TYPES[logits.dtype], stride, tokens, experts, top_k,
-                               _keep(keep, tokens), 1 if renormalize else 0, out.weight.data_ptr(),
-                               out.expert.data_ptr(), out.count.data_ptr(), out.offset.data_ptr(),
-                               out.slot.data_ptr(), out.place.data_ptr(), out._ws.data_ptr(), out._ws.numel(),
-                               _stream()), "hapmoe_route")
+                               _keep(keep, tokens), 1 if renormalize else 0, *out._outputs, _stream(logits)),
+           "hapmoe_route")
     return out
 
 
@@ -169,56 +183,60 @@ def route_backward(logits, routing: Routing, d_weight, keep=None, renormalize=Tr
     tokens, experts = logits.shape
     _need((routing.tokens, routing.experts) == (tokens, experts), "routing: made for other sizes")
     k = routing.top_k
-    _array("routing.expert", routing.expert, torch.int32, (tokens, k))
-    _array("routing.weight", routing.weight, torch.float32, (tokens, k))
-    _array("d_weight", d_weight, torch.float32, (tokens, k))
+    _array("routing.expert", routing.expert, torch.int32, tokens, k)
+    _array("routing.weight", routing.weight, torch.float32, tokens, k)
+    _array("d_weight", d_weight, torch.float32, tokens, k)
     d_logits = torch.empty((tokens, experts), dtype=logits.dtype, device=logits.device)
     _check(_lib().hapmoe_route_backward(logits.data_ptr(), _TYPES[logits.dtype], stride, tokens, experts, k,
                                         _keep(keep, tokens), 1 if renormalize else 0, routing.expert.data_ptr(),
                                         routing.weight.data_ptr(), d_weight.data_ptr(), d_logits.data_ptr(),
-                                        _stream()), "hapmoe_route_backward")
+                                        _stream(logits)), "hapmoe_route_backward")
     return d_logits
 
 
 # --------------------------------------------------- a token's expert outputs
+def _rows(name, t):
+    if _matrix(name, t, _TYPES) != t.shape[1]:
+        raise ValueError(f"{name}: contiguous")
+
+
+def _choices_of(place):
+    _array("place", place, torch.int32, None, None)
+    tokens, top_k = place.shape
+    if not 1 <= top_k <= MAX_TOP_K:
+        raise ValueError(f"place: 1 to {MAX_TOP_K} choices, not {top_k}")
+    return tokens, top_k
+
+
 def combine(y, place, weight=None):
     """out[t] = sum over j of weight[t, j] * y[place[t, j]] (``hapmoe_combine``); without weights, the sum:
     the gradient of the rows that ``expert_matmul`` gathers through slot."""
-    _on_device("y", y)
-    _need(y.dtype in _TYPES, f"y: a floating type of 32 or 16 bits, not {y.dtype}")
-    _array("y", y, y.dtype, (None, None))
-    _array("place", place, torch.int32, (None, None))
-    tokens, top_k = place.shape
-    _need(1 <= top_k <= MAX_TOP_K, f"place: up to {MAX_TOP_K} choices")
-    _need(y.shape[1] > 0, "y: no columns")
+    _rows("y", y)
+    tokens, top_k = _choices_of(place)
     if weight is not None:
-        _array("weight", weight, torch.float32, (tokens, top_k))
+        _array("weight", weight, torch.float32, tokens, top_k)
     out = torch.empty((tokens, y.shape[1]), dtype=y.dtype, device=y.device)
     _check(_lib().hapmoe_combine(y.data_ptr(), _TYPES[y.dtype], y.shape[0], tokens, top_k, y.shape[1],
                                  place.data_ptr(), None if weight is None else weight.data_ptr(), out.data_ptr(),
-                                 _stream()), "hapmoe_combine")
+                                 _stream(y)), "hapmoe_combine")
     return out
 
 
 def combine_backward(d_out, y, slot, place, weight):
     """The gradients (d_y [rows, hidden], d_weight [tokens, top_k] fp32) of ``combine`` from that of its result
     (``hapmoe_combine_backward``); rows = tokens * top_k."""
-    _on_device("y", y)
-    _need(y.dtype in _TYPES, f"y: a floating type of 32 or 16 bits, not {y.dtype}")
-    _array("place", place, torch.int32, (None, None))
-    tokens, top_k = place.shape
-    _need(1 <= top_k <= MAX_TOP_K, f"place: up to {MAX_TOP_K} choices")
-    _array("y", y, y.dtype, (tokens * top_k, None))
+    _rows("y", y)
+    tokens, top_k = _choices_of(place)
+    _array("y", y, y.dtype, tokens * top_k, None)
     hidden = y.shape[1]
-    _need(hidden > 0, "y: no columns")
-    _array("d_out", d_out, y.dtype, (tokens, hidden))
-    _array("slot", slot, torch.int32, (tokens * top_k,))
-    _array("weight", weight, torch.float32, (tokens, top_k))
+    _array("d_out", d_out, y.dtype, tokens, hidden)
+    _array("slot", slot, torch.int32, tokens * top_k)
+    _array("weight", weight, torch.float32, tokens, top_k)
     d_y = torch.empty_like(y)
     d_weight = torch.empty_like(weight)
     _check(_lib().hapmoe_combine_backward(d_out.data_ptr(), y.data_ptr(), _TYPES[y.dtype], tokens, top_k, hidden,
                                           slot.data_ptr(), place.data_ptr(), weight.data_ptr(), d_y.data_ptr(),
-                                          d_weight.data_ptr(), _stream()), "hapmoe_combine_backward")
+                                          d_weight.data_ptr(), _stream(y)), "hapmoe_combine_backward")
     return d_y, d_weight
 
 
@@ -229,14 +247,16 @@ _HALF = (torch.bfloat16, torch.float16)
 def _rows_of(x, slot):
     if slot is None:
         return x.shape[0]
-    _array("slot", slot, torch.int32, (None,))
+    _array("slot", slot, torch.int32, None)
     return slot.shape[0]
 
 
 def _experts_of(offset):
-    _array("offset", offset, torch.int32, (None,))
-    _need(1 <= offset.shape[0] - 1 <= MAX_EXPERTS, f"offset: 2 to {MAX_EXPERTS + 1} entries")
-    return offset.shape[0] - 1
+    _array("offset", offset, torch.int32, None)
+    experts = offset.shape[0] - 1
+    if not 1 <= experts <= MAX_EXPERTS:
+        raise ValueError(f"offset: 2 to {MAX_EXPERTS + 1} entries, not {experts + 1}")
+    return experts
 
 
 def expert_matmul(x, w, offset, slot=None, top_k=1):
@@ -245,13 +265,13 @@ def expert_matmul(x, w, offset, slot=None, top_k=1):
     x[slot[i] // top_k], as ``route`` orders them."""
     stride = _matrix("x", x, _HALF)
     experts = _experts_of(offset)
-    _array("w", w, x.dtype, (experts, None, x.shape[1]))
+    _array("w", w, x.dtype, experts, None, x.shape[1])
     _need(w.shape[1] > 0, "w: no outputs")
     rows = _rows_of(x, slot)
     y = torch.empty((rows, w.shape[1]), dtype=x.dtype, device=x.device)
     _check(_lib().hapmoe_expert_matmul(x.data_ptr(), x.shape[0], stride, w.data_ptr(), _TYPES[x.dtype], rows, experts,
                                        w.shape[1], w.shape[2], offset.data_ptr(),
-                                       None if slot is None else slot.data_ptr(), top_k, y.data_ptr(), _stream()),
+                                       None if slot is None else slot.data_ptr(), top_k, y.data_ptr(), _stream(x)),
            "hapmoe_expert_matmul")
     return y
 
@@ -261,12 +281,12 @@ def expert_matmul_grad_x(d_y, w, offset):
     through slot, ``combine(d_x, place)`` adds up those of each token."""
     stride = _matrix("d_y", d_y, _HALF)
     experts = _experts_of(offset)
-    _array("w", w, d_y.dtype, (experts, d_y.shape[1], None))
+    _array("w", w, d_y.dtype, experts, d_y.shape[1], None)
     _need(w.shape[2] > 0, "w: no inputs")
     d_x = torch.empty((d_y.shape[0], w.shape[2]), dtype=d_y.dtype, device=d_y.device)
     _check(_lib().hapmoe_expert_matmul_grad_x(d_y.data_ptr(), stride, w.data_ptr(), _TYPES[d_y.dtype], d_y.shape[0],
                                               experts, w.shape[1], w.shape[2], offset.data_ptr(), d_x.data_ptr(),
-                                              _stream()), "hapmoe_expert_matmul_grad_x")
+                                              _stream(d_y)), "hapmoe_expert_matmul_grad_x")
     return d_x
 
 
@@ -276,14 +296,17 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
     step = _matrix("d_y", d_y, _HALF)
     stride = _matrix("x", x, (d_y.dtype,))
     experts = _experts_of(offset)
-    _need(dtype in (torch.float32, d_y.dtype), f"dtype: torch.float32 or {d_y.dtype}, not {dtype}")
-    _need(_rows_of(x, slot) == d_y.shape[0], f"d_y: {_rows_of(x, slot)} rows, not {d_y.shape[0]}")
+    rows = _rows_of(x, slot)
+    if dtype not in (torch.float32, d_y.dtype):
+        raise ValueError(f"dtype: torch.float32 or {d_y.dtype}, not {dtype}")
+    if rows != d_y.shape[0]:
+        raise ValueError(f"d_y: {rows} rows, not {d_y.shape[0]}")
     d_w = torch.empty((experts, d_y.shape[1], x.shape[1]), dtype=dtype, device=x.device)
     _check(_lib().hapmoe_expert_matmul_grad_w(d_y.data_ptr(), step, x.data_ptr(), x.shape[0], stride,
-                                              _TYPES[x.dtype], x.shape[0] if slot is None else slot.shape[0], experts,
+                                              _TYPES[x.dtype], rows, experts,
                                               d_y.shape[1], x.shape[1], offset.data_ptr(),
                                               None if slot is None else slot.data_ptr(), top_k, _TYPES[dtype],
-                                              d_w.data_ptr(), _stream()), "hapmoe_expert_matmul_grad_w")
+                                              d_w.data_ptr(), _stream(x)), "hapmoe_expert_matmul_grad_w")
     return d_w
 
 
@@ -313,19 +336,19 @@ class AdamW:
         state = torch.float32 if self.state_bits == 32 else torch.uint8
         for i, p in enumerate(params):
             shape = tuple(p.shape)
-            _array(f"params[{i}]", p, torch.float32, shape)
+            _array(f"params[{i}]", p, torch.float32, *shape)
             for name, x in (("m", m), ("v", v)):
                 _need(x[i].numel() == p.numel(), f"{name}[{i}]: {p.numel()} elements, not {x[i].numel()}")
-                _array(f"{name}[{i}]", x[i], state, x[i].shape)
+                _array(f"{name}[{i}]", x[i], state, *x[i].shape)
             for name, x in (("m_exp", m_exp), ("v_exp", v_exp)):
                 if x is not None:
-                    _array(f"{name}[{i}]", x[i], torch.int8, (-(-p.numel() // BLOCK),))
+                    _array(f"{name}[{i}]", x[i], torch.int8, -(-p.numel() // BLOCK))
             if copies is not None:
                 _need(copies[i].dtype in _HALF and copies[i].dtype == copies[0].dtype,
                       f"copies[{i}]: all torch.bfloat16 or all torch.float16")
-                _array(f"copies[{i}]", copies[i], copies[0].dtype, shape)
+                _array(f"copies[{i}]", copies[i], copies[0].dtype, *shape)
             _need(decay[i] >= 0, f"weight_decay[{i}]: at least 0")
-        self.device = params[0].device if n else None
+        self._index = params[0].get_device() if n else None
         self._kept = (params, m, v, copies, m_exp, v_exp)
         self._sizes = [p.numel() for p in params]
         self._table = (_Tensor * max(n, 1))()
@@ -341,24 +364,27 @@ class AdamW:
         grad_scale multiplies the gradients.  seed: of the 8-bit moments' roundings, another for every step.
         skip: an int32 tensor of one element on the device; if it is not 0 nothing changes."""
         n = len(self._sizes)
-        _need(len(grads) == n, f"grads: {n}, not {len(grads)}")
+        if len(grads) != n:
+            raise ValueError(f"grads: {n}, not {len(grads)}")
         a, table = self._args, self._table
         if n:
-            dtype, device = grads[0].dtype, self.device
-            _need(dtype in _TYPES, f"grads: a floating type of 32 or 16 bits, not {dtype}")
-            _need(device.index == torch.cuda.current_device(), f"the parameters' {device} is not the current device")
+            dtype, index = grads[0].dtype, self._index
+            if dtype not in _TYPES:
+                raise ValueError(f"grads: a floating type of 32 or 16 bits, not {dtype}")
+            if index != torch.cuda.current_device():
+                raise ValueError(f"the parameters' device {index} is not the current device")
             for t, g, size in zip(table, grads, self._sizes):
-                if g.numel() != size or g.dtype != dtype or g.device != device or not g.is_contiguous():
-                    raise ValueError(f"grads: {size} contiguous elements of {dtype} on {device}, not "
+                if g.numel() != size or g.dtype != dtype or g.get_device() != index or not g.is_contiguous():
+                    raise ValueError(f"grads: {size} contiguous elements of {dtype} on device {index}, not "
                                      f"{tuple(g.shape)} of {g.dtype} on {g.device}")
                 t.grad = g.data_ptr()
             a.grad_type = _TYPES[dtype]
         a.lr, a.beta1, a.beta2, a.eps, a.grad_scale, a.step = lr, beta1, beta2, eps, grad_scale, step
         a.seed = seed & (2**64 - 1)
         if skip is not None:
-            _array("skip", skip, torch.int32, (1,))
+            _array("skip", skip, torch.int32, 1)
         a.d_skip = None if skip is None else skip.data_ptr()
-        _check(_lib().hapmoe_adamw(table, n, C.byref(a), _stream()), "hapmoe_adamw")
+        _check(_lib().hapmoe_adamw(table, n, C.byref(a), _stream_of(torch.cuda.current_device())), "hapmoe_adamw")
 
     def moments(self, dtype=torch.float32):
         """The values of m and v: two lists of tensors shaped like the parameters.  Moments in 8 bits are decoded
@@ -373,6 +399,6 @@ class AdamW:
             for p, code, exp in zip(params, codes, exps):
                 x = torch.empty(p.shape, dtype=dtype, device=p.device)
                 _check(_lib().hapmoe_adamw_moment(code.data_ptr(), exp.data_ptr(), p.numel(), second, _TYPES[dtype],
-                                                  x.data_ptr(), _stream()), "hapmoe_adamw_moment")
+                                                  x.data_ptr(), _stream(p)), "hapmoe_adamw_moment")
                 out[second].append(x)
         return out
