@@ -35,27 +35,6 @@ __device__ inline f32x4 mfma(s16x8 p, s16x8 q, f32x4 c, f16)
                                                   0);
 }
 
-// An operand as the kernels see it: element (i, k) of row i and summand k.  16-bit elements.
-// ALONG: memory runs along k, row i at base + row(i) * ld.  Otherwise across it, summand k at base + row(k) * ld.
-// row(): through slot (slot / top_k, none where that is past `rows`), or the number itself plus row0.
-struct Operand {
-    const short *base;
-    const int32_t *slot;
-    int64_t ld, row0;
-    int64_t rows;      // rows of the memory that exist
-    int top_k;
-    __device__ const short *row(int64_t i, int64_t most_slots) const
-    {
-        i += row0;
-        if (slot) {
-            if (i >= most_slots) return nullptr;
-            const int s = slot[i];
-            i = s < 0 ? rows : s / top_k;
-        }
-        return i < rows ? base + i * ld : nullptr;
-    }
-};
-
 // The rows of expert e, clamped to the rows that exist.
 __device__ inline int2 expert_rows(const int32_t *offset, int e, int64_t rows)
 {
@@ -128,27 +107,6 @@ __device__ inline bool find_tile(const int32_t *offset, int experts, int64_t row
     return false;
 }
 
-// ------------------------------------------------------------------ the kernel for any alignment
-// 128 x 128 outputs a workgroup of four waves (64 x 64 each), 64 summands at a time through registers into LDS.
-constexpr int kThreads = 256;
-constexpr int kB = 128;    // rows and columns
-constexpr int kK = 64;     // summands
-
-// 16 bytes from an address of any alignment, n of the 8 elements exist
-__device__ inline u32x4 load8(const short *p, int n)
-{
-    u32x4 x = {0, 0, 0, 0};
-    if (n >= 8) {
-        __builtin_memcpy(&x, p, 16);
-    } else if (n > 0) {
-        short s[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = i < n ? p[i] : 0;
-        __builtin_memcpy(&x, s, 16);
-    }
-    return x;
-}
-
 // LDS places (in 16-byte units) of a tile along k, [128][64], and across k, [64][128].  Along: row pairs take turns at
 // the eight places of a row, so 16 rows at one k lie in 16 different places of two rows' 256 bytes.  Across: rows k take
 // turns at the pairs of places, for the transposing read of rows 0-3, 8-11, ... of a 16-element column.
@@ -157,36 +115,6 @@ __device__ inline int across_place(int k, int c, int places)
 {
     return k * places + (c ^ (((k & 3) | ((k >> 1) & 4)) << 1 & (places - 1)));
 }
-
-template <bool ALONG>
-struct Stage {
-    u32x4 x[4];
-    // the thread's four 16-byte pieces of the tile at row i0, summand k0 (i_end rows, k_end summands exist)
-    __device__ void load(const Operand &o, int64_t i0, int64_t i_end, int64_t k0, int64_t k_end, int64_t most_slots)
-    {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int u = j * kThreads + threadIdx.x;
-            if constexpr (ALONG) {
-                const int64_t i = i0 + (u >> 3), k = k0 + (u & 7) * 8;
-                const short *r = i < i_end ? o.row(i, most_slots) : nullptr;
-                x[j] = r ? load8(r + k, (int)min((int64_t)8, k_end - k)) : u32x4{0, 0, 0, 0};
-            } else {
-                const int64_t k = k0 + (u >> 4), i = i0 + (u & 15) * 8;
-                const short *r = k < k_end ? o.row(k, most_slots) : nullptr;
-                x[j] = r ? load8(r + i, (int)min((int64_t)8, i_end - i)) : u32x4{0, 0, 0, 0};
-            }
-        }
-    }
-    __device__ void store(u32x4 *lds) const
-    {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int u = j * kThreads + threadIdx.x;
-            lds[ALONG ? along_place(u >> 3, u & 7) : across_place(u >> 4, u & 15, 16)] = x[j];
-        }
-    }
-};
 
 // The operand of a 16 x 16 x 32 product: row i0 + lane % 16, summands k0 + 8 (lane / 16) .. + 7.
 template <bool ALONG>
@@ -204,6 +132,15 @@ __device__ inline s16x8 fragment(const u32x4 *lds, int i0, int k0, int lane, int
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds *)b);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
+}
+
+enum { kForward, kGradX, kGradW };
+
+// the most tiles of b rows that `rows` rows of any split over the experts (and the rest) can have
+int64_t most_row_tiles(int64_t rows, int experts, int b)
+{
+    const int64_t parts = rows < experts + 1 ? rows : experts + 1;
+    return (rows - parts) / b + parts;
 }
 
 template <typename O>
@@ -224,108 +161,322 @@ __device__ inline void store_results(O *out, int n, f32x4 c)   // four neighbour
     }
 }
 
-enum { kForward, kGradX, kGradW };
+// The rank-th expert by falling number of rows, in classes of a power of two: the long sums begin first and the short
+// ones fill the gaps.  Every wave by itself, 64 experts a lane group.
+__device__ inline int expert_of_rank(const int32_t *offset, int experts, int64_t rows, int rank)
+{
+    constexpr int kGroups = HAPMOE_MAX_EXPERTS / 64;
+    const int lane = threadIdx.x & 63;
+    int size[kGroups], top = -1;   // class of the expert, -1 without rows, -2 past the last
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        size[g] = -2;
+        if (g * 64 >= experts) break;
+        const int e = g * 64 + lane;
+        if (e < experts) {
+            const int2 r = expert_rows(offset, e, rows);
+            size[g] = r.y > r.x ? 31 - __clz(r.y - r.x) : -1;
+        }
+        top = max(top, size[g]);
+    }
+    top = __builtin_amdgcn_readfirstlane(wave_reduce(top, Max()));
+    for (int c = top; c >= -1; --c) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            if (g * 64 >= experts) break;
+            uint64_t in = __ballot(size[g] == c);
+            const int n = __popcll(in);
+            if (rank < n) {
+                for (; rank > 0; --rank) in &= in - 1;
+                return g * 64 + __ffsll((unsigned long long)in) - 1;
+            }
+            rank -= n;
+        }
+    }
+    return 0;   // not reached: rank < experts
+}
 
-template <int KIND, typename T, typename O>
-__global__ __launch_bounds__(kThreads) void k_product_any(const ExpertProduct a, int p_tiles, int q_tiles)
+// The tile of a workgroup of d_w: the experts by falling number of rows, each one's tiles spread over the XCDs.  False for
+// one past an expert's tiles.
+__device__ inline bool find_grad_w_tile(const int32_t *offset, int experts, int64_t rows, int p_tiles, int q_tiles,
+                                        uint32_t block, Tile &t)
+{
+    const uint32_t tiles = (uint32_t)p_tiles * q_tiles, rounds = (tiles + 7) & ~7u;
+    const int id = (int)xcd_order(block % rounds, tiles);
+    if (id < 0) return false;
+    t.expert = expert_of_rank(offset, experts, rows, (int)(block / rounds));
+    t.q = id % q_tiles;
+    t.p = id / q_tiles;
+    const int2 r = expert_rows(offset, t.expert, rows);
+    t.lo = __builtin_amdgcn_readfirstlane(r.x);
+    t.hi = __builtin_amdgcn_readfirstlane(r.y);
+    return true;
+}
+int64_t grad_w_grid(int64_t experts, int64_t p_tiles, int64_t q_tiles)
+{
+    const int64_t grid = experts * (ceil_div(p_tiles * q_tiles, 8) * 8);
+    return p_tiles * q_tiles < 0x7ffffff0 ? grid : int64_t(1) << 40;
+}
+
+// ------------------------------------------------------------------ the kernel for any alignment
+// Rows that begin anywhere, any number of columns and summands: 16-byte loads of any alignment into registers, from there
+// into LDS.  B x B outputs a workgroup of four waves, 64 summands at a time, AHEAD tiles on their way: a tile's loads are
+// some 2 us under way, which is what bounds a product with few tiles.
+namespace any {
+
+constexpr int kThreads = 256;
+
+// n of the 8 elements at p, zeros for the others
+__device__ inline u32x4 load_some(const char *p, int n)
+{
+    short s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = i < n ? reinterpret_cast<const short *>(p)[i] : 0;
+    u32x4 x;
+    __builtin_memcpy(&x, s, 16);
+    return x;
+}
+// x without its first s elements, zeros behind them
+__device__ inline u32x4 drop(u32x4 x, int s)
+{
+    uint64_t lo = (uint64_t)x[1] << 32 | x[0], hi = (uint64_t)x[3] << 32 | x[2];
+    if (s >= 4) {
+        lo = hi;
+        hi = 0;
+    }
+    const int bits = (s & 3) * 16;
+    if (bits) {
+        lo = lo >> bits | hi << (64 - bits);
+        hi >>= bits;
+    }
+    if (s >= 8) lo = hi = 0;
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// One operand's tiles, kLoads pieces of 8 elements a thread.  fetch() is the load alone, of eight elements that exist;
+// fixed(), once it has landed, drops those before the piece and clears what does not exist.  SMALL: fewer than 8
+// columns or summands, element by element.
+template <bool ALONG, int SIDE, bool GATHER, bool SMALL>
+struct Loader {
+    static constexpr int kPlaces = ALONG ? 8 : SIDE / 8, kRows = kThreads / kPlaces, kLoads = SIDE / 32;
+    const char *row[ALONG ? kLoads : 1];   // along: of each piece; across: the thread's column of row 0
+    bool there[ALONG ? kLoads : 1];        // along: the row exists
+    int slots[ALONG ? 1 : kLoads];         // gathered across: of the next tile
+    const int32_t *slot;
+    int64_t ld2;
+    int first, shift, n, k_end, top_k, rows;
+
+    __device__ void begin(const void *memory, int64_t ld, const int32_t *all_slots, int k, int64_t row0,
+                          int64_t memory_rows, int64_t i0, int64_t i_end, int summands)
+    {
+        const auto *const bytes = static_cast<const char *>(memory);
+        const int r = threadIdx.x / kPlaces, c = threadIdx.x % kPlaces;
+        ld2 = ld * 2;
+        k_end = summands;
+        top_k = k;
+        rows = (int)memory_rows;
+        if constexpr (ALONG) {
+            first = c * 8;
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int64_t i = min(i0 + j * kRows + r, i_end - 1) + row0;   // results past the last go nowhere
+                int64_t from = i;
+                there[j] = true;
+                if constexpr (GATHER) {
+                    const int s = all_slots[i];
+                    there[j] = s >= 0 && s / top_k < rows;
+                    from = there[j] ? s / top_k : 0;
+                }
+                row[j] = bytes + from * ld2;
+            }
+        } else {
+            first = r;
+            const int64_t i = i0 + c * 8, from = SMALL ? min(i, i_end - 1) : min(i, i_end - 8);
+            n = (int)min((int64_t)8, max((int64_t)0, i_end - i));
+            shift = (int)(i - from);
+            row[0] = bytes + (GATHER ? 0 : row0 * ld2) + from * 2;
+            slot = GATHER ? all_slots + row0 : nullptr;
+            next_slots(0);
+        }
+    }
+    __device__ void next_slots(int tile)
+    {
+        if constexpr (!ALONG && GATHER) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) slots[j] = slot[min(tile * 64 + first + j * kRows, k_end - 1)];
+        }
+    }
+    // the loads of a tile, and what `fixed` has to know of gathered rows
+    __device__ void fetch(int tile, u32x4 *x, uint32_t &have)
+    {
+        have = 0;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const char *p;
+            int m = 8;
+            if constexpr (ALONG) {
+                const int k = tile * 64 + first;
+                p = row[j] + (int64_t)(SMALL ? min(k, k_end - 1) : min(k, k_end - 8)) * 2;
+                if constexpr (SMALL) m = k < k_end ? min(8, k_end - k) : 0;
+                have |= (uint32_t)there[j] << j;
+            } else {
+                int k = min(tile * 64 + first + j * kRows, k_end - 1);
+                bool ok = true;
+                if constexpr (GATHER) {
+                    ok = slots[j] >= 0 && slots[j] / top_k < rows;
+                    k = ok ? slots[j] / top_k : 0;
+                }
+                p = row[0] + k * ld2;
+                if constexpr (SMALL) m = n;
+                have |= (uint32_t)ok << j;
+            }
+            if constexpr (SMALL)
+                x[j] = load_some(p, m);
+            else
+                __builtin_memcpy(&x[j], p, 16);
+        }
+        next_slots(tile + 1);
+    }
+    __device__ void store(int tile, const u32x4 *x, uint32_t have, u32x4 *lds) const
+    {
+        const bool last = tile * 64 + 64 > k_end;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            u32x4 v = x[j];
+            const int r = threadIdx.x / kPlaces + j * kRows, c = threadIdx.x % kPlaces;
+            if constexpr (ALONG) {
+                const int k = tile * 64 + first;
+                if (!SMALL && last) v = drop(v, k - min(k, k_end - 8));
+            } else {
+                if (!SMALL && shift) v = drop(v, shift);
+                if (last && tile * 64 + r >= k_end) v = u32x4{0, 0, 0, 0};
+            }
+            if (GATHER && !(have >> j & 1)) v = u32x4{0, 0, 0, 0};
+            lds[ALONG ? along_place(r, c) : across_place(r, c, kPlaces)] = v;
+        }
+    }
+};
+
+template <int KIND, typename T, typename O, bool GATHER, bool SMALL, int B, int AHEAD>
+__global__ __launch_bounds__(kThreads, 2) void k_product(const ExpertProduct a, int p_tiles, int q_tiles)
 {
     constexpr bool kQAlong = KIND != kGradW, kPAlong = KIND == kForward;
-    __shared__ u32x4 lds_q[kB * kK / 8], lds_p[kB * kK / 8];
+    constexpr int kF = B / 32;   // a wave's fragments of each operand
+    __shared__ u32x4 lds_q[B * 8], lds_p[B * 8];
     Tile t;
-    Operand q, p;
-    int64_t q_end, p_end, k_end;
-    int64_t out_row;
+    Loader<kQAlong, B, GATHER && KIND == kForward, SMALL> lq;
+    Loader<kPAlong, B, GATHER && KIND == kGradW, SMALL> lp;
+    int64_t q_end, p_end, out_row;
+    int k_end;
     if constexpr (KIND == kGradW) {
-        const int64_t id = xcd_order(blockIdx.x, (int64_t)a.experts * p_tiles * q_tiles);
-        if (id < 0) return;
-        t.expert = (int)(id / ((int64_t)p_tiles * q_tiles));
-        const int local = (int)(id % ((int64_t)p_tiles * q_tiles));
-        t.q = local % q_tiles;
-        t.p = local / q_tiles;
-        const int2 r = expert_rows(a.offset, t.expert, a.rows);
-        q = Operand{static_cast<const short *>(a.d_y), nullptr, a.d_y_stride, r.x, a.rows, 1};
-        p = Operand{static_cast<const short *>(a.x), a.slot, a.x_stride, r.x, a.x_rows, a.top_k};
+        if (!find_grad_w_tile(a.offset, a.experts, a.rows, p_tiles, q_tiles, blockIdx.x, t)) return;
         q_end = a.outputs;
         p_end = a.inputs;
-        k_end = r.y - r.x;
+        k_end = t.hi - t.lo;
         out_row = (int64_t)t.expert * a.outputs;
+        if (k_end > 0) {
+            lq.begin(a.d_y, a.d_y_stride, nullptr, 1, t.lo, a.rows, (int64_t)t.q * B, q_end, k_end);
+            lp.begin(a.x, a.x_stride, a.slot, a.top_k, t.lo, a.x_rows, (int64_t)t.p * B, p_end, k_end);
+        }
+        if (GATHER && a.x_rows == 0) k_end = 0;
     } else {
-        if (!find_tile<kB>(a.offset, a.experts, a.rows, p_tiles, blockIdx.x, t)) return;
-        const int64_t ld = KIND == kForward ? a.x_stride : a.d_y_stride;
-        q = Operand{static_cast<const short *>(KIND == kForward ? a.x : a.d_y), KIND == kForward ? a.slot : nullptr, ld,
-                    t.lo, KIND == kForward ? a.x_rows : a.rows, a.top_k};
-        const int64_t e = t.expert < a.experts ? t.expert : 0;
-        p = Operand{static_cast<const short *>(a.w) + e * a.outputs * a.inputs, nullptr, a.inputs, 0, a.outputs, 1};
+        if (!find_tile<B>(a.offset, a.experts, a.rows, p_tiles, blockIdx.x, t)) return;
         q_end = t.hi - t.lo;
         p_end = KIND == kForward ? a.outputs : a.inputs;
-        k_end = t.expert < a.experts ? (KIND == kForward ? a.inputs : a.outputs) : 0;
+        k_end = t.expert == a.experts ? 0 : KIND == kForward ? (int)a.inputs : (int)a.outputs;
+        if (GATHER && a.x_rows == 0) k_end = 0;
         out_row = t.lo;
-    }
-    const int64_t q0 = (int64_t)t.q * kB, p0 = (int64_t)t.p * kB;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wq = (wave >> 1) * 64, wp = (wave & 1) * 64;
-    f32x4 acc[4][4] = {};
-    Stage<kQAlong> sq;
-    Stage<kPAlong> sp;
-    if (k_end > 0) {
-        sq.load(q, q0, q_end, 0, k_end, a.rows);
-        sp.load(p, p0, p_end, 0, k_end, a.rows);
-    }
-    for (int64_t k0 = 0; k0 < k_end; k0 += kK) {
-        __syncthreads();
-        sq.store(lds_q);
-        sp.store(lds_p);
-        __syncthreads();
-        if (k0 + kK < k_end) {
-            sq.load(q, q0, q_end, k0 + kK, k_end, a.rows);
-            sp.load(p, p0, p_end, k0 + kK, k_end, a.rows);
+        if (k_end > 0) {
+            const char *w = static_cast<const char *>(a.w) + t.expert * a.outputs * a.inputs * 2;
+            lq.begin(KIND == kForward ? a.x : a.d_y, KIND == kForward ? a.x_stride : a.d_y_stride, a.slot, a.top_k, t.lo,
+                     KIND == kForward ? a.x_rows : a.rows, (int64_t)t.q * B, q_end, k_end);
+            lp.begin(w, a.inputs, nullptr, 1, 0, a.outputs, (int64_t)t.p * B, p_end, k_end);
         }
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wq = (wave >> 1) * (B / 2), wp = (wave & 1) * (B / 2);
+    const int tiles = (k_end + 63) >> 6;
+    f32x4 acc[kF][kF] = {};
+    u32x4 xq[AHEAD][decltype(lq)::kLoads], xp[AHEAD][decltype(lp)::kLoads];
+    uint32_t hq[AHEAD], hp[AHEAD];
 #pragma unroll
-        for (int k = 0; k < kK; k += 32) {
-            s16x8 fq[4], fp[4];
+    for (int d = 0; d < AHEAD; ++d)
+        if (d < tiles) {
+            lq.fetch(d, xq[d], hq[d]);
+            lp.fetch(d, xp[d], hp[d]);
+        }
+    for (int t0 = 0; t0 < tiles; t0 += AHEAD) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                fq[i] = fragment<kQAlong>(lds_q, wq + 16 * i, k, lane, 16);
-                fp[i] = fragment<kPAlong>(lds_p, wp + 16 * i, k, lane, 16);
+        for (int d = 0; d < AHEAD; ++d) {
+            const int tile = t0 + d;
+            if (tile >= tiles) break;
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the tile before is read
+            lq.store(tile, xq[d], hq[d], lds_q);
+            lp.store(tile, xp[d], hp[d], lds_p);
+            if (tile + AHEAD < tiles) {
+                lq.fetch(tile + AHEAD, xq[d], hq[d]);
+                lp.fetch(tile + AHEAD, xp[d], hp[d]);
             }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this one is written
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int k = 0; k < 64; k += 32) {
+                s16x8 fq[kF], fp[kF];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = mfma(fp[j], fq[i], acc[i][j], T());
+                for (int i = 0; i < kF; ++i) {
+                    fq[i] = fragment<kQAlong>(lds_q, wq + 16 * i, k, lane, B / 8);
+                    fp[i] = fragment<kPAlong>(lds_p, wp + 16 * i, k, lane, B / 8);
+                }
+#pragma unroll
+                for (int i = 0; i < kF; ++i)
+#pragma unroll
+                    for (int j = 0; j < kF; ++j) acc[i][j] = mfma(fp[j], fq[i], acc[i][j], T());
+            }
         }
     }
     O *out = static_cast<O *>(a.out);
+    const int64_t q0 = (int64_t)t.q * B + wq, p0 = (int64_t)t.p * B + wp;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = q0 + wq + 16 * i + (lane & 15);
+    for (int i = 0; i < kF; ++i) {
+        const int64_t r = q0 + 16 * i + (lane & 15);
         if (r >= q_end) continue;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = p0 + wp + 16 * j + (lane >> 4) * 4;
+        for (int j = 0; j < kF; ++j) {
+            const int64_t c = p0 + 16 * j + (lane >> 4) * 4;
             if (c < p_end) store_results(out + (out_row + r) * p_end + c, (int)min((int64_t)4, p_end - c), acc[i][j]);
         }
     }
 }
 
-// the most tiles of b rows that `rows` rows of any split over the experts (and the rest) can have
-int64_t most_row_tiles(int64_t rows, int experts, int b)
+template <int KIND, typename T, typename O, bool GATHER, bool SMALL, int B, int AHEAD>
+hipError_t launch(const ExpertProduct &a, hipStream_t s)
 {
-    const int64_t parts = rows < experts + 1 ? rows : experts + 1;
-    return (rows - parts) / b + parts;
+    const int64_t p_tiles = ceil_div(KIND == kForward ? a.outputs : a.inputs, B), q_tiles = ceil_div(a.outputs, B);
+    const int64_t tiles = KIND == kGradW ? grad_w_grid(a.experts, p_tiles, q_tiles)
+                                         : most_row_tiles(a.rows, a.experts, B) * p_tiles;
+    const int64_t grid = ceil_div(tiles, 8) * 8;   // whole rounds of the XCDs
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_product<KIND, T, O, GATHER, SMALL, B, AHEAD>), dim3((unsigned)grid), dim3(kThreads), 0, s, a,
+                       (int)p_tiles, (int)q_tiles);
+    return hipGetLastError();
+}
+
+template <int KIND, typename T, typename O, bool GATHER>
+hipError_t by_size(const ExpertProduct &a, hipStream_t s)
+{
+    if (a.inputs < 8 || a.outputs < 8) return launch<KIND, T, O, GATHER, true, 64, 1>(a, s);
+    const int64_t p_size = KIND == kForward ? a.outputs : a.inputs;
+    const int64_t tiles = ceil_div(KIND == kGradW ? a.experts * a.outputs : a.rows, 128) * ceil_div(p_size, 128);
+    if (tiles < 1024) return launch<KIND, T, O, GATHER, false, 64, 4>(a, s);
+    return launch<KIND, T, O, GATHER, false, 128, 2>(a, s);
 }
 
 template <int KIND, typename T, typename O>
-hipError_t product_any(const ExpertProduct &a, hipStream_t s)
+hipError_t product(const ExpertProduct &a, hipStream_t s)
 {
-    const int64_t p_size = KIND == kForward ? a.outputs : a.inputs;
-    const int64_t p_tiles = ceil_div(p_size, kB), q_tiles = ceil_div(a.outputs, kB);
-    const int64_t tiles = KIND == kGradW ? a.experts * p_tiles * q_tiles : most_row_tiles(a.rows, a.experts, kB) * p_tiles;
-    const int64_t grid = ceil_div(tiles, 8) * 8;   // whole rounds of the XCDs
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_product_any<KIND, T, O>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, (int)p_tiles,
-                       (int)q_tiles);
-    return hipGetLastError();
+    return a.slot && KIND != kGradX ? by_size<KIND, T, O, true>(a, s) : by_size<KIND, T, O, false>(a, s);
 }
+
+}  // namespace any
 
 // ------------------------------------------------------------------ the kernel for whole vectors
 // Rows and columns that begin on 16 bytes, columns and summands in eights.  The loads go from memory straight into LDS
@@ -535,41 +686,6 @@ struct Fragments {
     }
 };
 
-// The rank-th expert by falling number of rows, in classes of a power of two: the long sums begin first and the short
-// ones fill the gaps.  Every wave by itself, 64 experts a lane group.
-__device__ inline int expert_of_rank(const int32_t *offset, int experts, int64_t rows, int rank)
-{
-    constexpr int kGroups = HAPMOE_MAX_EXPERTS / 64;
-    const int lane = threadIdx.x & 63;
-    int size[kGroups], top = -1;   // class of the expert, -1 without rows, -2 past the last
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        size[g] = -2;
-        if (g * 64 >= experts) break;
-        const int e = g * 64 + lane;
-        if (e < experts) {
-            const int2 r = expert_rows(offset, e, rows);
-            size[g] = r.y > r.x ? 31 - __clz(r.y - r.x) : -1;
-        }
-        top = max(top, size[g]);
-    }
-    top = __builtin_amdgcn_readfirstlane(wave_reduce(top, Max()));
-    for (int c = top; c >= -1; --c) {
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            if (g * 64 >= experts) break;
-            uint64_t in = __ballot(size[g] == c);
-            const int n = __popcll(in);
-            if (rank < n) {
-                for (; rank > 0; --rank) in &= in - 1;
-                return g * 64 + __ffsll((unsigned long long)in) - 1;
-            }
-            rank -= n;
-        }
-    }
-    return 0;   // not reached: rank < experts
-}
-
 // The results of a workgroup's waves to rows q0 .. q_end of out, columns p0 .. p_end.  LDS is read by now: it takes them,
 // as many rows at a time as fit, and they leave it as whole rows of the tile.  A row's places are turned by its number,
 // so that neither the 16 rows of a write nor a row's read meet in a bank.
@@ -631,21 +747,14 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
     int64_t q_end, p_end, out_row;
     int k_end;
     if constexpr (KIND == kGradW) {
-        const int tiles = args.p_tiles * args.q_tiles, rounds = (tiles + 7) & ~7;
-        const int id = (int)xcd_order(blockIdx.x % rounds, tiles);
-        if (id < 0) return;
-        t.expert = expert_of_rank(a.offset, a.experts, a.rows, blockIdx.x / rounds);
-        t.q = id % args.q_tiles;
-        t.p = id / args.q_tiles;
-        const int2 r = expert_rows(a.offset, t.expert, a.rows);
+        if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, blockIdx.x, t)) return;
         q_end = a.outputs;
         p_end = a.inputs;
-        k_end = __builtin_amdgcn_readfirstlane(r.y - r.x);
-        const int lo = __builtin_amdgcn_readfirstlane(r.x);
+        k_end = t.hi - t.lo;
         out_row = (int64_t)t.expert * a.outputs;
         if (k_end > 0) {
-            lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, lo, a.rows, (int64_t)t.q * BQ, q_end, k_end);
-            lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, lo, a.x_rows, (int64_t)t.p * BP, p_end, k_end);
+            lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, t.lo, a.rows, (int64_t)t.q * BQ, q_end, k_end);
+            lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, t.lo, a.x_rows, (int64_t)t.p * BP, p_end, k_end);
         }
     } else {
         if (!find_tile<BQ>(a.offset, a.experts, a.rows, args.p_tiles, blockIdx.x, t)) return;
@@ -787,13 +896,10 @@ __global__ __launch_bounds__(256, 2) void k_grad_w(const Args args)
     constexpr int kFq = BQ / kWQ / 16, kFp = BP / kWP / 16;
     __shared__ u32x4 lds[kStages * (kTileQ + kTileP)];
     const ExpertProduct &a = args.a;
-    const int per = args.p_tiles * args.q_tiles, rounds = (per + 7) & ~7;
-    const int id = (int)xcd_order(blockIdx.x % rounds, per);
-    if (id < 0) return;
-    const int expert = expert_of_rank(a.offset, a.experts, a.rows, blockIdx.x / rounds);
-    const int64_t q0 = (int64_t)(id % args.q_tiles) * BQ, p0 = (int64_t)(id / args.q_tiles) * BP;
-    const int2 range = expert_rows(a.offset, expert, a.rows);
-    const int lo = __builtin_amdgcn_readfirstlane(range.x), k_end = __builtin_amdgcn_readfirstlane(range.y) - lo;
+    Tile t;
+    if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, blockIdx.x, t)) return;
+    const int64_t q0 = (int64_t)t.q * BQ, p0 = (int64_t)t.p * BP;
+    const int k_end = t.hi - t.lo;
     Loader<false, BQ, kThreads, false, kDepth> lq;
     Loader<false, BP, kThreads, GATHER, kDepth> lp;
     constexpr int kLoadsQ = decltype(lq)::kLoads, kLoads = kLoadsQ + decltype(lp)::kLoads;
@@ -821,8 +927,8 @@ __global__ __launch_bounds__(256, 2) void k_grad_w(const Args args)
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
     if (tiles > 0) {
-        lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, lo, a.rows, q0, a.outputs, k_end);
-        lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, lo, a.x_rows, p0, a.inputs, k_end);
+        lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, t.lo, a.rows, q0, a.outputs, k_end);
+        lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, t.lo, a.x_rows, p0, a.inputs, k_end);
         issue(0);
         if (tiles > 1) issue(1);
     }
@@ -868,7 +974,7 @@ __global__ __launch_bounds__(256, 2) void k_grad_w(const Args args)
     }
     for (; i < tiles; ++i, turn()) step(std::integral_constant<int, 0>(), i, stage);
     store_tile<O, BQ, BP, kWQ, kWP, kStages * (kTileQ + kTileP)>(
-        lds, acc, static_cast<O *>(a.out) + expert * a.outputs * a.inputs, q0, a.outputs, p0, a.inputs);
+        lds, acc, static_cast<O *>(a.out) + t.expert * a.outputs * a.inputs, q0, a.outputs, p0, a.inputs);
 }
 
 template <int KIND, typename T, typename O, int BQ, int BP, int WQ, int WP, int STAGES>
@@ -879,10 +985,10 @@ hipError_t launch(const ExpertProduct &a, hipStream_t s)
     args.by_top_k = divisor(a.slot ? a.top_k : 1);
     args.p_tiles = (int)ceil_div(KIND == kForward ? a.outputs : a.inputs, BP);
     args.q_tiles = (int)ceil_div(a.outputs, BQ);
-    const int64_t tiles = KIND == kGradW ? a.experts * (ceil_div((int64_t)args.p_tiles * args.q_tiles, 8) * 8)
+    const int64_t tiles = KIND == kGradW ? grad_w_grid(a.experts, args.p_tiles, args.q_tiles)
                                          : most_row_tiles(a.rows, a.experts, BQ) * args.p_tiles;
     const int64_t grid = ceil_div(tiles, 8) * 8;
-    if (grid > 0x7fffffff || (int64_t)args.p_tiles * args.q_tiles > 0x7ffffff0) return hipErrorInvalidValue;
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
     constexpr int kThreads = 64 * WQ * WP;
     if (a.slot && KIND != kGradX)
         hipLaunchKernelGGL((k_product<KIND, T, O, true, BQ, BP, WQ, WP, STAGES>), dim3((unsigned)grid), dim3(kThreads),
@@ -901,8 +1007,7 @@ hipError_t launch_grad_w(const ExpertProduct &a, hipStream_t s)
     args.by_top_k = divisor(a.slot ? a.top_k : 1);
     args.p_tiles = (int)ceil_div(a.inputs, BP);
     args.q_tiles = (int)ceil_div(a.outputs, BQ);
-    const int64_t per = (int64_t)args.p_tiles * args.q_tiles;
-    const int64_t grid = a.experts * (ceil_div(per, 8) * 8);   // whole rounds of the XCDs for each expert
+    const int64_t grid = grad_w_grid(a.experts, args.p_tiles, args.q_tiles);
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
     hipLaunchKernelGGL((a.slot ? k_grad_w<T, O, true, BQ, BP> : k_grad_w<T, O, false, BQ, BP>), dim3((unsigned)grid),
                        dim3(256), 0, s, args);
@@ -936,7 +1041,7 @@ bool whole_vectors(const ExpertProduct &a)
 template <int KIND, typename T, typename O>
 hipError_t product(const ExpertProduct &a, hipStream_t s)
 {
-    return whole_vectors(a) ? fast::product<KIND, T, O>(a, s) : product_any<KIND, T, O>(a, s);
+    return whole_vectors(a) ? fast::product<KIND, T, O>(a, s) : any::product<KIND, T, O>(a, s);
 }
 
 }  // namespace
