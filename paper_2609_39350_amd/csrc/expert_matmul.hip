@@ -143,21 +143,67 @@ int64_t most_row_tiles(int64_t rows, int experts, int b)
     return (rows - parts) / b + parts;
 }
 
-template <typename O>
-__device__ inline void store_results(O *out, int n, f32x4 c)   // four neighbours, n of them exist
+// All but this wave's last LOADS loads into LDS have landed, its LDS reads are done, and so for every wave.
+template <int LOADS>
+__device__ inline void sync_tiles()
 {
-    struct Four {
-        O v[4];
-    };
-    Four f;
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+}
+
+// The results of a workgroup's waves to rows q0 .. q_end of out, columns p0 .. p_end.  LDS is read by now: it takes them,
+// as many rows at a time as fit, and they leave it as whole rows of the tile.  A row's places are turned by its number,
+// so that neither the 16 rows of a write nor a row's read meet in a bank.
+// WHOLE: rows and columns begin and end on 16 bytes.
+template <typename O, int BQ, int BP, int WQ, int WP, int SPACE, bool WHOLE = true>
+__device__ inline void store_tile(u32x4 *lds, const f32x4 (&acc)[BQ / WQ / 16][BP / WP / 16], O *out, int64_t q0,
+                                  int64_t q_end, int64_t p0, int64_t p_end)
+{
+    constexpr int kThreads = 64 * WQ * WP, kFq = BQ / WQ / 16, kFp = BP / WP / 16;
+    constexpr int kOut = 16 / (int)sizeof(O);                 // results in 16 bytes
+    constexpr int kRow = BP / kOut;                           // places of a row
+    constexpr int kRounds = BQ * kRow <= SPACE ? 1 : 2;
+    constexpr int kPart = kFq / kRounds * 16;                 // a wave's rows of a round
+    static_assert(BQ / kRounds * kRow <= SPACE && kFq % kRounds == 0, "the results' LDS");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = (wave % WP) * (BP / WP);
+    char *const bytes = reinterpret_cast<char *>(lds);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f.v[i] = from_f32<O>(c[i]);
-    if (n >= 4) {
-        __builtin_memcpy(out, &f, sizeof(f));
-    } else {
+    for (int h = 0; h < kRounds; ++h) {
+        sync_tiles<0>();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) out[i] = f.v[i];
+        for (int i = 0; i < kPart / 16; ++i) {
+            const int r = wave / WP * kPart + 16 * i + (lane & 15);
+#pragma unroll
+            for (int j = 0; j < kFp; ++j) {
+                const int c = wp + 16 * j + (lane >> 4) * 4;
+                struct alignas(4 * sizeof(O)) Four {
+                    O v[4];
+                } f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f.v[k] = from_f32<O>(acc[h * (kPart / 16) + i][j][k]);
+                *reinterpret_cast<Four *>(bytes + (r * kRow + (c / kOut ^ (r & (kRow - 1)))) * 16 +
+                                          c % kOut * (int)sizeof(O)) = f;
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll 4
+        for (int u = threadIdx.x; u < BQ / kRounds * kRow; u += kThreads) {
+            const int r = u / kRow, c = u % kRow;
+            const int64_t q = q0 + r / kPart * (BQ / WQ) + h * kPart + r % kPart, p = p0 + c * kOut;
+            if (q >= q_end || p >= p_end) continue;
+            const u32x4 x = lds[r * kRow + (c ^ (r & (kRow - 1)))];
+            O *const to = out + q * p_end + p;
+            if constexpr (WHOLE) {
+                *reinterpret_cast<u32x4 *>(to) = x;
+            } else if (p + kOut <= p_end) {
+                __builtin_memcpy(to, &x, 16);
+            } else {
+                O v[kOut];
+                __builtin_memcpy(v, &x, 16);
+#pragma unroll
+                for (int i = 0; i < kOut; ++i)
+                    if (p + i < p_end) to[i] = v[i];
+            }
+        }
     }
 }
 
@@ -362,7 +408,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_product(const ExpertProduct a, 
 {
     constexpr bool kQAlong = KIND != kGradW, kPAlong = KIND == kForward;
     constexpr int kF = B / 32;   // a wave's fragments of each operand
-    __shared__ u32x4 lds_q[B * 8], lds_p[B * 8];
+    __shared__ u32x4 lds[2 * B * 8];
+    u32x4 *const lds_q = lds, *const lds_p = lds + B * 8;
     Tile t;
     Loader<kQAlong, B, GATHER && KIND == kForward, SMALL> lq;
     Loader<kPAlong, B, GATHER && KIND == kGradW, SMALL> lp;
@@ -433,18 +480,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_product(const ExpertProduct a, 
             }
         }
     }
-    O *out = static_cast<O *>(a.out);
-    const int64_t q0 = (int64_t)t.q * B + wq, p0 = (int64_t)t.p * B + wp;
-#pragma unroll
-    for (int i = 0; i < kF; ++i) {
-        const int64_t r = q0 + 16 * i + (lane & 15);
-        if (r >= q_end) continue;
-#pragma unroll
-        for (int j = 0; j < kF; ++j) {
-            const int64_t c = p0 + 16 * j + (lane >> 4) * 4;
-            if (c < p_end) store_results(out + (out_row + r) * p_end + c, (int)min((int64_t)4, p_end - c), acc[i][j]);
-        }
-    }
+    store_tile<O, B, B, 2, 2, 2 * B * 8, false>(lds, acc, static_cast<O *>(a.out) + out_row * p_end, (int64_t)t.q * B, q_end,
+                                                (int64_t)t.p * B, p_end);
 }
 
 template <int KIND, typename T, typename O, bool GATHER, bool SMALL, int B, int AHEAD>
@@ -532,13 +569,6 @@ __device__ inline void touch(const char *base, uint32_t offset, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(scalar(base)), "s"(to)
                  : "memory");
-}
-
-// All but this wave's last LOADS loads into LDS have landed, its LDS reads are done, and so for every wave.
-template <int LOADS>
-__device__ inline void sync_tiles()
-{
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
 }
 
 // One operand's tiles: kLoads pieces of 16 bytes for each of THREADS threads.
@@ -685,50 +715,6 @@ struct Fragments {
         for (int i = 0; i < N; ++i) f[i] = fragment<ALONG>(tile, i0 + 16 * i, k, lane, places);
     }
 };
-
-// The results of a workgroup's waves to rows q0 .. q_end of out, columns p0 .. p_end.  LDS is read by now: it takes them,
-// as many rows at a time as fit, and they leave it as whole rows of the tile.  A row's places are turned by its number,
-// so that neither the 16 rows of a write nor a row's read meet in a bank.
-template <typename O, int BQ, int BP, int WQ, int WP, int SPACE>
-__device__ inline void store_tile(u32x4 *lds, const f32x4 (&acc)[BQ / WQ / 16][BP / WP / 16], O *out, int64_t q0,
-                                  int64_t q_end, int64_t p0, int64_t p_end)
-{
-    constexpr int kThreads = 64 * WQ * WP, kFq = BQ / WQ / 16, kFp = BP / WP / 16;
-    constexpr int kOut = 16 / (int)sizeof(O);                 // results in 16 bytes
-    constexpr int kRow = BP / kOut;                           // places of a row
-    constexpr int kRounds = BQ * kRow <= SPACE ? 1 : 2;
-    constexpr int kPart = kFq / kRounds * 16;                 // a wave's rows of a round
-    static_assert(BQ / kRounds * kRow <= SPACE && kFq % kRounds == 0, "the results' LDS");
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = (wave % WP) * (BP / WP);
-    char *const bytes = reinterpret_cast<char *>(lds);
-#pragma unroll
-    for (int h = 0; h < kRounds; ++h) {
-        sync_tiles<0>();
-#pragma unroll
-        for (int i = 0; i < kPart / 16; ++i) {
-            const int r = wave / WP * kPart + 16 * i + (lane & 15);
-#pragma unroll
-            for (int j = 0; j < kFp; ++j) {
-                const int c = wp + 16 * j + (lane >> 4) * 4;
-                struct alignas(4 * sizeof(O)) Four {
-                    O v[4];
-                } f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) f.v[k] = from_f32<O>(acc[h * (kPart / 16) + i][j][k]);
-                *reinterpret_cast<Four *>(bytes + (r * kRow + (c / kOut ^ (r & (kRow - 1)))) * 16 +
-                                          c % kOut * (int)sizeof(O)) = f;
-            }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll 4
-        for (int u = threadIdx.x; u < BQ / kRounds * kRow; u += kThreads) {
-            const int r = u / kRow, c = u % kRow;
-            const int64_t q = q0 + r / kPart * (BQ / WQ) + h * kPart + r % kPart, p = p0 + c * kOut;
-            if (q < q_end && p < p_end)
-                *reinterpret_cast<u32x4 *>(out + q * p_end + p) = lds[r * kRow + (c ^ (r & (kRow - 1)))];
-        }
-    }
-}
 
 // BQ x BP outputs a workgroup of WQ x WP waves.  STAGES tiles of 64 summands in LDS.
 template <int KIND, typename T, typename O, bool GATHER, int BQ, int BP, int WQ, int WP, int STAGES>
