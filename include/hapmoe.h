@@ -559,14 +559,13 @@ int32_t hapmoe_expert_matmul_grad_w(const void *d_d_y, int64_t d_y_stride, const
  * one power of two for every 256 elements (ceil(n / 256) exponents each). */
 typedef struct hapmoe_adamw_tensor {
     float *param;        /* fp32 master */
-    const void *grad;
     void *copy;          /* 16-bit copy of the updated master, or NULL (in all tensors with n > 0, or in none) */
     void *m, *v;
     int8_t *m_exp, *v_exp;   /* state_bits = 8 only */
     int64_t n;
     float weight_decay;
     int32_t reserved;    /* 0 */
-} hapmoe_adamw_tensor;   /* 72 bytes */
+} hapmoe_adamw_tensor;   /* 64 bytes */
 
 typedef struct hapmoe_adamw_args {
     double lr, beta1, beta2, eps;
@@ -580,8 +579,8 @@ typedef struct hapmoe_adamw_args {
     int32_t reserved;        /* 0 */
 } hapmoe_adamw_args;
 
-/* AdamW over n_tensors tensors (host arrays of structs, read before the call
- * returns), in place:
+/* AdamW over n_tensors tensors and their gradients (host arrays, of structs and
+ * of device pointers, read before the call returns), in place:
  *   g = grad_scale grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   param -= lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps) + lr weight_decay param
  * all in fp32.  With state_bits = 8 the fresh m and v enter the step; then they
@@ -593,13 +592,14 @@ typedef struct hapmoe_adamw_args {
  * the running means do not drift or stick; a v above 0 stays above 0.  The 16
  * random bits of each are a fixed function of seed and of the element's index
  * over all tensors, each counted in whole blocks of 256. */
-int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, int32_t n_tensors, const hapmoe_adamw_args *args,
-                     void *stream);
+int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, const void *const *grads, int32_t n_tensors,
+                     const hapmoe_adamw_args *args, void *stream);
 
-/* The values that n elements of an 8-bit moment stand for, as fp32 or bf16
- * (exact in both, but for bf16's subnormals): second = 0 for m, 1 for v. */
-int32_t hapmoe_adamw_moment(const uint8_t *d_code, const int8_t *d_exp, int64_t n, int32_t second, int32_t out_type,
-                            void *d_out, void *stream);
+/* The values that the 8-bit moments of n_tensors tensors stand for, as fp32 or
+ * bf16 (exact in both, but for bf16's subnormals): d_m[i] and d_v[i] are device
+ * arrays of the i-th tensor's n elements. */
+int32_t hapmoe_adamw_moments(const hapmoe_adamw_tensor *tensors, void *const *d_m, void *const *d_v, int32_t n_tensors,
+                             int32_t out_type, void *stream);
 
 #ifdef __cplusplus
 }

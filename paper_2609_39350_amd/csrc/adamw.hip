@@ -1,7 +1,7 @@
 // AdamW over many tensors, moments in fp32 or in 8 bits.  Bound by HBM: every
 // operand is read once and written once.  The tensors' addresses travel in the
 // kernel's arguments (up to kTensors a launch), so a step copies nothing to the
-// device and may be captured; a workgroup takes kChunk elements of one tensor.
+// device and may be captured.
 //
 // Every operation is a single fp32 one, rounded to nearest (no contraction), in
 // the order of the formula in the header.
@@ -11,7 +11,12 @@ namespace hapmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 4096;
+constexpr int kRound = 4 * kThreads;   // elements of a workgroup at a time
+// A call over more elements than this streams: 4 rounds a workgroup and non-temporal loads and stores, for nothing is
+// read twice in a step and little of it stays in the last cache (256 MB) until the next.  268 M elements in fp32 with a bf16
+// copy: 1,510 us without, 1,426 with (5.33 -> 5.65 TB/s); but 9.6 M (288 MB), step after step: 47 without, 58 with.
+constexpr int64_t kStream = int64_t(1) << 24;
+constexpr int rounds_of(bool stream) { return stream ? 4 : 1; }
 constexpr int kBlock = 256;    // elements that share an exponent: four a lane of a wave
 constexpr int kTensors = 40;
 
@@ -36,7 +41,8 @@ struct Batch {
 };
 static_assert(sizeof(Batch) <= 4096, "kernel arguments");
 
-__device__ inline int entry_of(const Batch &b, uint32_t chunk)
+template <typename B>
+__device__ inline int entry_of(const B &b, uint32_t chunk)
 {
     int lo = 0, hi = b.count - 1;
     while (lo < hi) {
@@ -49,16 +55,33 @@ __device__ inline int entry_of(const Batch &b, uint32_t chunk)
     return lo;
 }
 
+// Four elements of a type, as words.
+template <typename T>
+using Words = uint32_t __attribute__((ext_vector_type(sizeof(T))));
+template <bool STREAM, typename W>
+__device__ inline W load(const W *p)
+{
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
+}
+template <bool STREAM, typename W>
+__device__ inline void store(W x, W *p)
+{
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(x, p);
+    else
+        *p = x;
+}
+
 // Four consecutive elements; n of them exist where the tensor ends or its vectors are not aligned (VEC false).
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool STREAM>
 __device__ inline void load4(float *x, const void *p, int64_t i, int n)
 {
     const T *q = static_cast<const T *>(p) + i;
     if constexpr (VEC) {
-        struct alignas(4 * sizeof(T)) Four {
+        struct Four {
             T v[4];
         };
-        const Four f = *reinterpret_cast<const Four *>(q);
+        const Four f = __builtin_bit_cast(Four, load<STREAM>(reinterpret_cast<const Words<T> *>(q)));
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = to_f32(f.v[k]);
     } else {
@@ -66,40 +89,40 @@ __device__ inline void load4(float *x, const void *p, int64_t i, int n)
         for (int k = 0; k < 4; ++k) x[k] = k < n ? to_f32(q[k]) : 0.0f;
     }
 }
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool STREAM>
 __device__ inline void store4(void *p, int64_t i, int n, const float *x)
 {
     T *q = static_cast<T *>(p) + i;
     if constexpr (VEC) {
-        struct alignas(4 * sizeof(T)) Four {
+        struct Four {
             T v[4];
         };
         Four f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) f.v[k] = from_f32<T>(x[k]);
-        *reinterpret_cast<Four *>(q) = f;
+        store<STREAM>(__builtin_bit_cast(Words<T>, f), reinterpret_cast<Words<T> *>(q));
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (k < n) q[k] = from_f32<T>(x[k]);
     }
 }
-template <bool VEC>
+template <bool VEC, bool STREAM>
 __device__ inline uint32_t load_codes(const void *p, int64_t i, int n)
 {
     const uint8_t *q = static_cast<const uint8_t *>(p) + i;
-    if constexpr (VEC) return *reinterpret_cast<const uint32_t *>(q);
+    if constexpr (VEC) return load<STREAM>(reinterpret_cast<const uint32_t *>(q));
     uint32_t c = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) c |= k < n ? (uint32_t)q[k] << 8 * k : 0u;
     return c;
 }
-template <bool VEC>
+template <bool VEC, bool STREAM>
 __device__ inline void store_codes(void *p, int64_t i, int n, uint32_t c)
 {
     uint8_t *q = static_cast<uint8_t *>(p) + i;
     if constexpr (VEC) {
-        *reinterpret_cast<uint32_t *>(q) = c;
+        store<STREAM>(c, reinterpret_cast<uint32_t *>(q));
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -145,23 +168,23 @@ __device__ inline uint32_t random32(uint64_t seed, uint64_t i)
 
 __device__ inline int exponent_field(float x) { return (int)(__builtin_bit_cast(uint32_t, x) >> 23 & 255); }
 
-template <typename G, typename C, int BITS, bool VEC>
+template <typename G, typename C, int BITS, bool VEC, bool STREAM>
 __device__ inline void update(const Batch &b, const Entry &t, int64_t i, int n)
 {
     // with BITS 8 every lane of the wave takes part in the maxima, those past the end with zeros
     float p[4], g[4], m[4], v[4];
     if (n > 0) {
-        load4<float, VEC>(p, t.param, i, n);
-        load4<G, VEC>(g, t.grad, i, n);
+        load4<float, VEC, STREAM>(p, t.param, i, n);
+        load4<G, VEC, STREAM>(g, t.grad, i, n);
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) p[k] = g[k] = 0.0f;
     }
     if constexpr (BITS == 32) {
-        load4<float, VEC>(m, t.m, i, n);
-        load4<float, VEC>(v, t.v, i, n);
+        load4<float, VEC, STREAM>(m, t.m, i, n);
+        load4<float, VEC, STREAM>(v, t.v, i, n);
     } else {
-        const uint32_t cm = n > 0 ? load_codes<VEC>(t.m, i, n) : 0, cv = n > 0 ? load_codes<VEC>(t.v, i, n) : 0;
+        const uint32_t cm = n > 0 ? load_codes<VEC, STREAM>(t.m, i, n) : 0, cv = n > 0 ? load_codes<VEC, STREAM>(t.v, i, n) : 0;
         const int64_t block = n > 0 ? i / kBlock : 0;
         const float sm = power_of_two(t.m_exp[block]), sv = power_of_two(t.v_exp[block]);
 #pragma unroll
@@ -178,12 +201,12 @@ __device__ inline void update(const Batch &b, const Entry &t, int64_t i, int n)
         p[k] = p[k] - (m[k] * b.size / (sqrtf(v[k]) * b.root + b.eps) + t.decay * p[k]);
     }
     if (n > 0) {
-        store4<float, VEC>(t.param, i, n, p);
-        if constexpr (sizeof(C) == 2) store4<C, VEC>(t.copy, i, n, p);
+        store4<float, VEC, STREAM>(t.param, i, n, p);
+        if constexpr (sizeof(C) == 2) store4<C, VEC, STREAM>(t.copy, i, n, p);
     }
     if constexpr (BITS == 32) {
-        store4<float, VEC>(t.m, i, n, m);
-        store4<float, VEC>(t.v, i, n, v);
+        store4<float, VEC, STREAM>(t.m, i, n, m);
+        store4<float, VEC, STREAM>(t.v, i, n, v);
     } else {
         int em = 0, ev = 0;
 #pragma unroll
@@ -208,8 +231,8 @@ __device__ inline void update(const Batch &b, const Entry &t, int64_t i, int n)
             x = v[k] > 0.0f && x == 0 ? 1u : x;
             cv |= x << 8 * k;
         }
-        store_codes<VEC>(t.m, i, n, cm);
-        store_codes<VEC>(t.v, i, n, cv);
+        store_codes<VEC, STREAM>(t.m, i, n, cm);
+        store_codes<VEC, STREAM>(t.v, i, n, cv);
         if ((threadIdx.x & 63) == 0) {
             t.m_exp[i / kBlock] = (int8_t)em;
             t.v_exp[i / kBlock] = (int8_t)ev;
@@ -217,68 +240,103 @@ __device__ inline void update(const Batch &b, const Entry &t, int64_t i, int n)
     }
 }
 
-template <typename G, typename C, int BITS>
+template <typename G, typename C, int BITS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_adamw(const Batch b)
 {
     if (b.skip && *b.skip) return;
+    constexpr int kRounds = rounds_of(STREAM);
     const uint32_t chunk = blockIdx.x;
     const Entry &t = b.t[entry_of(b, chunk)];
-    const int64_t lo = (int64_t)(chunk - (t.chunk0 & 0x7fffffffu)) * kChunk;
-    const bool vec = t.chunk0 >> 31 && lo + kChunk <= t.n;
+    const int64_t lo = (int64_t)(chunk - (t.chunk0 & 0x7fffffffu)) * kRounds * kRound;
+    const bool vec = t.chunk0 >> 31 && lo + kRounds * kRound <= t.n;
 #pragma unroll 2
-    for (int r = 0; r < kChunk / (4 * kThreads); ++r) {
-        const int64_t i = lo + (int64_t)(r * kThreads + threadIdx.x) * 4;
-        const int64_t left = t.n - i;
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = lo + r * kRound + threadIdx.x * 4, left = t.n - i;
         if (vec)
-            update<G, C, BITS, true>(b, t, i, 4);
+            update<G, C, BITS, true, STREAM>(b, t, i, 4);
         else if (BITS == 8 || left > 0)
-            update<G, C, BITS, false>(b, t, i, left > 4 ? 4 : left < 0 ? 0 : (int)left);
+            update<G, C, BITS, false, STREAM>(b, t, i, left > 4 ? 4 : left < 0 ? 0 : (int)left);
     }
 }
 
 template <typename G, typename C>
-void launch(const Batch &b, int bits, hipStream_t s)
+void launch(const Batch &b, int bits, bool stream, hipStream_t s)
 {
-    if (bits == 32)
-        hipLaunchKernelGGL((k_adamw<G, C, 32>), dim3(b.chunks), dim3(kThreads), 0, s, b);
-    else
-        hipLaunchKernelGGL((k_adamw<G, C, 8>), dim3(b.chunks), dim3(kThreads), 0, s, b);
+    auto *kernel = bits == 32 ? (stream ? k_adamw<G, C, 32, true> : k_adamw<G, C, 32, false>)
+                              : (stream ? k_adamw<G, C, 8, true> : k_adamw<G, C, 8, false>);
+    hipLaunchKernelGGL(kernel, dim3(b.chunks), dim3(kThreads), 0, s, b);
 }
 template <typename G>
-void launch(const Batch &b, int copy_type, int bits, hipStream_t s)   // copy_type F32: none
+void launch(const Batch &b, int copy_type, int bits, bool stream, hipStream_t s)   // copy_type F32: none
 {
     if (copy_type == HAPMOE_F32)
-        launch<G, float>(b, bits, s);
+        launch<G, float>(b, bits, stream, s);
     else if (copy_type == HAPMOE_BF16)
-        launch<G, bf16>(b, bits, s);
+        launch<G, bf16>(b, bits, stream, s);
     else
-        launch<G, f16>(b, bits, s);
+        launch<G, f16>(b, bits, stream, s);
 }
 
-template <int BIAS, typename T>
-__global__ __launch_bounds__(kThreads) void k_moment(const uint8_t *__restrict__ code, const int8_t *__restrict__ exp,
-                                                     int64_t n, int vec, T *__restrict__ out)
+// Both moments of up to kTensors tensors as values, a wave a block of 256 elements at a time.
+struct Moment {
+    const uint8_t *m, *v;
+    const int8_t *m_exp, *v_exp;
+    void *out_m, *out_v;
+    int64_t n;
+    uint32_t chunk0;   // as in Entry
+};
+struct Moments {
+    int32_t count;
+    uint32_t chunks;
+    Moment t[kTensors];
+};
+static_assert(sizeof(Moments) <= 4096, "kernel arguments");
+
+template <int BIAS, typename T, bool VEC, bool STREAM>
+__device__ inline void expand(const uint8_t *code, const int8_t *exp, void *out, int64_t i, int n)
 {
-    const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
-    if (i >= n) return;
-    const int left = n - i > 4 ? 4 : (int)(n - i);
+    const uint32_t c = load_codes<VEC, STREAM>(code, i, n);
     const float scale = power_of_two(exp[i / kBlock]);
-    const bool whole = vec && left == 4;
-    const uint32_t c = whole ? load_codes<true>(code, i, 4) : load_codes<false>(code, i, left);
     float x[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = decode<BIAS>(c >> 8 * k & 255) * scale;
-    if (whole)
-        store4<T, true>(out, i, 4, x);
-    else
-        store4<T, false>(out, i, left, x);
+    store4<T, VEC, STREAM>(out, i, n, x);
+}
+
+template <typename T, bool STREAM>
+__global__ __launch_bounds__(kThreads) void k_moments(const Moments b)
+{
+    constexpr int kRounds = rounds_of(STREAM);
+    const Moment &t = b.t[entry_of(b, blockIdx.x)];
+    const int64_t lo = (int64_t)(blockIdx.x - (t.chunk0 & 0x7fffffffu)) * kRounds * kRound;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = lo + r * kRound + threadIdx.x * 4, left = t.n - i;
+        if (left <= 0) return;
+        if (t.chunk0 >> 31 && left >= 4) {
+            expand<7, T, true, STREAM>(t.m, t.m_exp, t.out_m, i, 4);
+            expand<15, T, true, STREAM>(t.v, t.v_exp, t.out_v, i, 4);
+        } else {
+            expand<7, T, false, STREAM>(t.m, t.m_exp, t.out_m, i, left > 4 ? 4 : (int)left);
+            expand<15, T, false, STREAM>(t.v, t.v_exp, t.out_v, i, left > 4 ? 4 : (int)left);
+        }
+    }
+}
+
+bool streams(const hapmoe_adamw_tensor *tensors, int n)
+{
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) total += tensors[i].n;
+    return total > kStream;
 }
 
 }  // namespace
 
-hipError_t launch_adamw(const hapmoe_adamw_tensor *tensors, int n, const hapmoe_adamw_args &a, hipStream_t s)
+hipError_t launch_adamw(const hapmoe_adamw_tensor *tensors, const void *const *grads, int n, const hapmoe_adamw_args &a,
+                        hipStream_t s)
 {
     Batch b;
+    const bool stream = streams(tensors, n);
     b.beta1 = (float)a.beta1;
     b.rest1 = (float)(1.0 - a.beta1);
     b.beta2 = (float)a.beta2;
@@ -298,12 +356,12 @@ hipError_t launch_adamw(const hapmoe_adamw_tensor *tensors, int n, const hapmoe_
         int copy_type = HAPMOE_F32;
         for (; i < n && b.count < kTensors; ++i) {
             const hapmoe_adamw_tensor &x = tensors[i];
-            const int64_t chunks = ceil_div(x.n, kChunk);
+            const int64_t chunks = ceil_div(x.n, rounds_of(stream) * kRound);
             if (x.n == 0) continue;
             if (b.count && b.chunks + chunks > 0x7fffffff) break;
             Entry &t = b.t[b.count++];
             t.param = x.param;
-            t.grad = x.grad;
+            t.grad = grads[i];
             t.copy = x.copy;
             t.m = x.m;
             t.v = x.v;
@@ -312,7 +370,7 @@ hipError_t launch_adamw(const hapmoe_adamw_tensor *tensors, int n, const hapmoe_
             t.n = x.n;
             t.first = first;
             t.decay = x.weight_decay * (float)a.lr;
-            const bool vec = aligned(x.param, 16) && aligned(x.grad, 4 * grad_bytes) && aligned(x.copy, 8) &&
+            const bool vec = aligned(x.param, 16) && aligned(grads[i], 4 * grad_bytes) && aligned(x.copy, 8) &&
                              aligned(x.m, a.state_bits == 32 ? 16 : 4) && aligned(x.v, a.state_bits == 32 ? 16 : 4);
             t.chunk0 = b.chunks | (vec ? 0x80000000u : 0);
             b.chunks += (uint32_t)chunks;
@@ -321,28 +379,41 @@ hipError_t launch_adamw(const hapmoe_adamw_tensor *tensors, int n, const hapmoe_
         }
         if (b.count == 0) break;
         if (a.grad_type == HAPMOE_F32)
-            launch<float>(b, copy_type, a.state_bits, s);
+            launch<float>(b, copy_type, a.state_bits, stream, s);
         else if (a.grad_type == HAPMOE_BF16)
-            launch<bf16>(b, copy_type, a.state_bits, s);
+            launch<bf16>(b, copy_type, a.state_bits, stream, s);
         else
-            launch<f16>(b, copy_type, a.state_bits, s);
+            launch<f16>(b, copy_type, a.state_bits, stream, s);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
 }
 
-hipError_t launch_adamw_moment(const uint8_t *code, const int8_t *exp, int64_t n, bool second, int out_type, void *out,
-                               hipStream_t s)
+hipError_t launch_adamw_moments(const hapmoe_adamw_tensor *tensors, void *const *out_m, void *const *out_v, int n,
+                                int out_type, hipStream_t s)
 {
-    const unsigned grid = (unsigned)ceil_div(n, 4 * kThreads);
-    const int vec = aligned(code, 4) && aligned(out, 4 * type_bytes(out_type));
-    if (out_type == HAPMOE_F32)
-        hipLaunchKernelGGL((second ? k_moment<15, float> : k_moment<7, float>), dim3(grid), dim3(kThreads), 0, s, code,
-                           exp, n, vec, static_cast<float *>(out));
-    else
-        hipLaunchKernelGGL((second ? k_moment<15, bf16> : k_moment<7, bf16>), dim3(grid), dim3(kThreads), 0, s, code,
-                           exp, n, vec, static_cast<bf16 *>(out));
-    return hipGetLastError();
+    Moments b;
+    const bool stream = streams(tensors, n);
+    for (int i = 0; i < n;) {
+        b.count = 0;
+        b.chunks = 0;
+        for (; i < n && b.count < kTensors; ++i) {
+            const hapmoe_adamw_tensor &x = tensors[i];
+            if (x.n == 0) continue;
+            const int64_t chunks = ceil_div(x.n, rounds_of(stream) * kRound), bytes = 4 * type_bytes(out_type);
+            if (b.count && b.chunks + chunks > 0x7fffffff) break;
+            const bool vec = aligned(x.m, 4) && aligned(x.v, 4) && aligned(out_m[i], bytes) && aligned(out_v[i], bytes);
+            b.t[b.count++] = Moment{static_cast<const uint8_t *>(x.m), static_cast<const uint8_t *>(x.v), x.m_exp, x.v_exp,
+                                    out_m[i], out_v[i], x.n, b.chunks | (vec ? 0x80000000u : 0)};
+            b.chunks += (uint32_t)chunks;
+        }
+        if (b.count == 0) break;
+        auto *kernel = out_type == HAPMOE_F32 ? (stream ? k_moments<float, true> : k_moments<float, false>)
+                                              : (stream ? k_moments<bf16, true> : k_moments<bf16, false>);
+        hipLaunchKernelGGL(kernel, dim3(b.chunks), dim3(kThreads), 0, s, b);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace hapmoe

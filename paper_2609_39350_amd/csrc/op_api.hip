@@ -159,10 +159,10 @@ int32_t hapmoe_expert_matmul_grad_w(const void *d_d_y, int64_t d_y_stride, const
     return status(launch_expert_matmul_grad_w(a, (hipStream_t)stream));
 }
 
-int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, int32_t n_tensors, const hapmoe_adamw_args *args,
-                     void *stream)
+int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, const void *const *grads, int32_t n_tensors,
+                     const hapmoe_adamw_args *args, void *stream)
 {
-    if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !args) return HAPMOE_E_INVAL;
+    if (n_tensors < 0 || (n_tensors > 0 && (!tensors || !grads)) || !args) return HAPMOE_E_INVAL;
     const hapmoe_adamw_args &a = *args;
     if (!any_type(a.grad_type) || (a.state_bits != 32 && a.state_bits != 8) || a.step < 1) return HAPMOE_E_INVAL;
     if (!(std::isfinite(a.lr) && a.lr >= 0.0) || !(a.beta1 >= 0.0 && a.beta1 < 1.0) ||
@@ -178,24 +178,29 @@ int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, int32_t n_tensors, cons
         if (t.n == 0) continue;
         if (copies < 0) copies = t.copy != nullptr;
         if ((t.copy != nullptr) != (copies == 1) || (t.copy && !half_type(a.copy_type))) return HAPMOE_E_INVAL;
-        if (!t.param || !t.grad || !t.m || !t.v || (a.state_bits == 8 && (!t.m_exp || !t.v_exp))) return HAPMOE_E_INVAL;
-        if (!aligned(t.param, 4) || !element_aligned(t.grad, a.grad_type) || !aligned(t.copy, 2)) return HAPMOE_E_INVAL;
+        if (!t.param || !grads[i] || !t.m || !t.v || (a.state_bits == 8 && (!t.m_exp || !t.v_exp))) return HAPMOE_E_INVAL;
+        if (!aligned(t.param, 4) || !element_aligned(grads[i], a.grad_type) || !aligned(t.copy, 2)) return HAPMOE_E_INVAL;
         if (a.state_bits == 32 && (!aligned(t.m, 4) || !aligned(t.v, 4))) return HAPMOE_E_INVAL;
     }
     if (const int e = check_arch()) return e;
-    return status(launch_adamw(tensors, n_tensors, a, (hipStream_t)stream));
+    return status(launch_adamw(tensors, grads, n_tensors, a, (hipStream_t)stream));
 }
 
-int32_t hapmoe_adamw_moment(const uint8_t *d_code, const int8_t *d_exp, int64_t n, int32_t second, int32_t out_type,
-                            void *d_out, void *stream)
+int32_t hapmoe_adamw_moments(const hapmoe_adamw_tensor *tensors, void *const *d_m, void *const *d_v, int32_t n_tensors,
+                             int32_t out_type, void *stream)
 {
-    if (n < 0 || n > kMaxElements || second < 0 || second > 1 || (out_type != HAPMOE_F32 && out_type != HAPMOE_BF16))
-        return HAPMOE_E_INVAL;
-    if (n > 0 && (!d_code || !d_exp || !d_out || !element_aligned(d_out, out_type))) return HAPMOE_E_INVAL;
-    if (n > (int64_t(1) << 40)) return HAPMOE_E_INVAL;   // the grid
+    if (n_tensors < 0 || (n_tensors > 0 && (!tensors || !d_m || !d_v))) return HAPMOE_E_INVAL;
+    if (out_type != HAPMOE_F32 && out_type != HAPMOE_BF16) return HAPMOE_E_INVAL;
+    int64_t total = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const hapmoe_adamw_tensor &t = tensors[i];
+        if (t.n < 0 || t.n > kMaxElements || (total += t.n) > kMaxElements) return HAPMOE_E_INVAL;
+        if (t.n == 0) continue;
+        if (!t.m || !t.v || !t.m_exp || !t.v_exp || !d_m[i] || !d_v[i]) return HAPMOE_E_INVAL;
+        if (!element_aligned(d_m[i], out_type) || !element_aligned(d_v[i], out_type)) return HAPMOE_E_INVAL;
+    }
     if (const int e = check_arch()) return e;
-    if (n == 0) return HAPMOE_OK;
-    return status(launch_adamw_moment(d_code, d_exp, n, second != 0, out_type, d_out, (hipStream_t)stream));
+    return status(launch_adamw_moments(tensors, d_m, d_v, n_tensors, out_type, (hipStream_t)stream));
 }
 
 }  // extern "C"

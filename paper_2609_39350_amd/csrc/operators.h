@@ -44,9 +44,10 @@ hipError_t launch_expert_matmul(const ExpertProduct &a, hipStream_t s);
 hipError_t launch_expert_matmul_grad_x(const ExpertProduct &a, hipStream_t s);
 hipError_t launch_expert_matmul_grad_w(const ExpertProduct &a, hipStream_t s);
 
-hipError_t launch_adamw(const hapmoe_adamw_tensor *t, int n, const hapmoe_adamw_args &a, hipStream_t s);
-hipError_t launch_adamw_moment(const uint8_t *code, const int8_t *exp, int64_t n, bool second, int out_type, void *out,
-                               hipStream_t s);
+hipError_t launch_adamw(const hapmoe_adamw_tensor *t, const void *const *grads, int n, const hapmoe_adamw_args &a,
+                        hipStream_t s);
+hipError_t launch_adamw_moments(const hapmoe_adamw_tensor *t, void *const *out_m, void *const *out_v, int n,
+                                int out_type, hipStream_t s);
 
 #ifdef __HIPCC__
 // Eight elements, 16 bytes of a 16-bit type or 32 of fp32.

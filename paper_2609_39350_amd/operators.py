@@ -31,7 +31,7 @@ _LIB = None
 
 
 class _Tensor(C.Structure):
-    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p),
+    _fields_ = [("param", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p),
                 ("v", C.c_void_p), ("m_exp", C.c_void_p), ("v_exp", C.c_void_p), ("n", C.c_int64),
                 ("weight_decay", C.c_float), ("reserved", C.c_int32)]
 
@@ -58,8 +58,8 @@ def _lib():
                 "hapmoe_expert_matmul_grad_x": [vp, i64, vp, i32, i64, i32, i64, i64, vp, vp, vp],
                 "hapmoe_expert_matmul_grad_w": [vp, i64, vp, i64, i64, i32, i64, i32, i64, i64, vp, vp, i32, i32, vp,
                                                 vp],
-                "hapmoe_adamw": [C.POINTER(_Tensor), i32, C.POINTER(_Args), vp],
-                "hapmoe_adamw_moment": [vp, vp, i64, i32, i32, vp, vp]}.items():
+                "hapmoe_adamw": [C.POINTER(_Tensor), vp, i32, C.POINTER(_Args), vp],
+                "hapmoe_adamw_moments": [C.POINTER(_Tensor), vp, vp, i32, i32, vp]}.items():
             f = getattr(L, name)
             f.argtypes, f.restype = args, i32
         _LIB = L
@@ -311,6 +311,9 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
 
 
 # -------------------------------------------------------------- the optimizer
+_POINTER, _CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.is_contiguous
+
+
 class AdamW:
     """AdamW over the caller's tensors, in place (``hapmoe_adamw``).
 
@@ -352,6 +355,7 @@ class AdamW:
         self._kept = (params, m, v, copies, m_exp, v_exp)
         self._sizes = [p.numel() for p in params]
         self._table = (_Tensor * max(n, 1))()
+        self._pointers = C.c_void_p * max(n, 1)
         self._args = _Args(copy_type=_TYPES[copies[0].dtype] if copies else 0, state_bits=self.state_bits)
         for i, t in enumerate(self._table[:n]):
             t.param, t.m, t.v, t.n = params[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr(), params[i].numel()
@@ -366,39 +370,45 @@ class AdamW:
         n = len(self._sizes)
         if len(grads) != n:
             raise ValueError(f"grads: {n}, not {len(grads)}")
-        a, table = self._args, self._table
+        a = self._args
         if n:
             dtype, index = grads[0].dtype, self._index
             if dtype not in _TYPES:
                 raise ValueError(f"grads: a floating type of 32 or 16 bits, not {dtype}")
             if index != torch.cuda.current_device():
                 raise ValueError(f"the parameters' device {index} is not the current device")
-            for t, g, size in zip(table, grads, self._sizes):
-                if g.numel() != size or g.dtype != dtype or g.get_device() != index or not g.is_contiguous():
-                    raise ValueError(f"grads: {size} contiguous elements of {dtype} on device {index}, not "
-                                     f"{tuple(g.shape)} of {g.dtype} on {g.device}")
-                t.grad = g.data_ptr()
+            # list by list: a step over many small tensors waits for these checks
+            if ([g.dtype for g in grads].count(dtype) != n or [g.get_device() for g in grads].count(index) != n
+                    or [g.numel() for g in grads] != self._sizes or not all(map(_CONTIGUOUS, grads))):
+                raise ValueError(f"grads: contiguous on device {index}, of one type and the parameters' sizes")
             a.grad_type = _TYPES[dtype]
         a.lr, a.beta1, a.beta2, a.eps, a.grad_scale, a.step = lr, beta1, beta2, eps, grad_scale, step
         a.seed = seed & (2**64 - 1)
         if skip is not None:
             _array("skip", skip, torch.int32, 1)
         a.d_skip = None if skip is None else skip.data_ptr()
-        _check(_lib().hapmoe_adamw(table, n, C.byref(a), _stream_of(torch.cuda.current_device())), "hapmoe_adamw")
+        _check(_lib().hapmoe_adamw(self._table, self._pointers(*map(_POINTER, grads)), n, C.byref(a),
+                                   _stream_of(torch.cuda.current_device())), "hapmoe_adamw")
 
     def moments(self, dtype=torch.float32):
         """The values of m and v: two lists of tensors shaped like the parameters.  Moments in 8 bits are decoded
-        to fp32 or bf16 (``hapmoe_adamw_moment``); fp32 ones are the state's own tensors."""
-        params, m, v, _, m_exp, v_exp = self._kept
+        to fp32 or bf16 (``hapmoe_adamw_moments``); fp32 ones are the state's own tensors."""
+        params, m, v = self._kept[:3]
         if self.state_bits == 32:
             _need(dtype == torch.float32, "moments in 32 bits are torch.float32")
             return list(m), list(v)
         _need(dtype in (torch.float32, torch.bfloat16), f"dtype: torch.float32 or torch.bfloat16, not {dtype}")
-        out = ([], [])
-        for second, (codes, exps) in enumerate(((m, m_exp), (v, v_exp))):
-            for p, code, exp in zip(params, codes, exps):
-                x = torch.empty(p.shape, dtype=dtype, device=p.device)
-                _check(_lib().hapmoe_adamw_moment(code.data_ptr(), exp.data_ptr(), p.numel(), second, _TYPES[dtype],
-                                                  x.data_ptr(), _stream(p)), "hapmoe_adamw_moment")
-                out[second].append(x)
+        if params and self._index != torch.cuda.current_device():
+            raise ValueError(f"the parameters' device {self._index} is not the current device")
+        # one allocation, cut at multiples of 8 elements
+        starts, total = [], 0
+        for n in self._sizes * 2:
+            starts.append(total)
+            total += -(-n // 8) * 8
+        flat = torch.empty(total, dtype=dtype, device=f"cuda:{self._index or 0}")
+        pieces = [flat.as_strided(p.shape, p.stride(), at) for p, at in zip(params + params, starts)]
+        out = pieces[:len(params)], pieces[len(params):]
+        _check(_lib().hapmoe_adamw_moments(self._table, *(self._pointers(*map(_POINTER, x)) for x in out), len(params),
+                                           _TYPES[dtype], _stream_of(torch.cuda.current_device())),
+               "hapmoe_adamw_moments")
         return out

@@ -23,7 +23,7 @@ def changed(base, **by_index):
 
 
 def test_struct_sizes():
-    assert C.sizeof(ops._Tensor) == 72 and C.sizeof(ops._Args) == 80
+    assert C.sizeof(ops._Tensor) == 64 and C.sizeof(ops._Args) == 80
 
 
 def test_route():
@@ -78,35 +78,50 @@ def test_expert_products():
         assert L.hapmoe_expert_matmul_grad_w(*changed(good, **{f"a{i}": v})) == INVAL, (i, v)
 
 
-def adamw(tensor=(), **args):
+def adamw(tensor=(), grad=P, **args):
     t = (ops._Tensor * 2)()
     for x in t:
-        x.param = x.grad = x.m = x.v = P
+        x.param = x.m = x.v = P
         x.n = 100
     for k, v in dict(tensor).items():
         setattr(t[1], k, v)
     a = ops._Args(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, grad_scale=1.0, step=1, state_bits=32)
     for k, v in args.items():
         setattr(a, k, v)
-    return ops._lib().hapmoe_adamw(t, 2, C.byref(a), None)
+    return ops._lib().hapmoe_adamw(t, (C.c_void_p * 2)(P, grad), 2, C.byref(a), None)
 
 
 def test_adamw():
     assert adamw() in NO_DEVICE
     assert adamw({"n": 0, "param": None, "copy": P}) in NO_DEVICE
-    for bad in ({"n": -1}, {"param": None}, {"grad": None}, {"m": None}, {"v": None}, {"param": P + 2}, {"m": P + 1},
+    for bad in ({"n": -1}, {"param": None}, {"m": None}, {"v": None}, {"param": P + 2}, {"m": P + 1},
                 {"copy": P}, {"weight_decay": -0.1}, {"weight_decay": math.inf}, {"n": 2**60}):
         assert adamw(bad) == INVAL, bad
     for bad in ({"lr": -1.0}, {"lr": math.nan}, {"beta1": 1.0}, {"beta2": -0.1}, {"eps": -1.0}, {"step": 0},
                 {"grad_scale": math.inf}, {"grad_type": 5}, {"state_bits": 16}, {"state_bits": 8}, {"d_skip": P + 1}):
         assert adamw(**bad) == INVAL, bad
+    assert adamw(grad=None) == INVAL and adamw(grad=P + 1) == INVAL
     f = ops._lib().hapmoe_adamw
-    assert f(None, 1, None, None) == INVAL and f(None, -1, C.byref(ops._Args()), None) == INVAL
-    good = [P, P, 100, 1, ops.BF16, P, None]
-    f = ops._lib().hapmoe_adamw_moment
-    assert f(*good) in NO_DEVICE
-    for i, v in ((0, None), (1, None), (2, -1), (3, 2), (4, ops.F16), (5, None), (5, P + 1)):
-        assert f(*changed(good, **{f"a{i}": v})) == INVAL, (i, v)
+    assert f(None, None, 1, None, None) == INVAL and f(None, None, -1, C.byref(ops._Args()), None) == INVAL
+
+
+def test_adamw_moments():
+    f = ops._lib().hapmoe_adamw_moments
+
+    def call(tensor=(), m=P, v=P, out_type=ops.BF16, n=2):
+        t = (ops._Tensor * 2)()
+        for x in t:
+            x.m = x.v = x.m_exp = x.v_exp = P
+            x.n = 100
+        for k, value in dict(tensor).items():
+            setattr(t[1], k, value)
+        return f(t, (C.c_void_p * 2)(P, m), (C.c_void_p * 2)(P, v), n, out_type, None)
+
+    assert call() in NO_DEVICE and call(m=None, v=None, tensor={"n": 0}) in NO_DEVICE
+    for bad in ({"m": None}, {"v": None}, {"m": P + 1}, {"out_type": ops.F16}, {"n": -1}, {"tensor": {"n": -1}},
+                {"tensor": {"m": None}}, {"tensor": {"v_exp": None}}, {"tensor": {"n": 2**60}}):
+        assert call(**bad) == INVAL, bad
+    assert f(None, None, None, 1, ops.F32, None) == INVAL
 
 
 def test_wrong_tensors_raise_value_error():
