@@ -69,7 +69,7 @@ __device__ inline T from_f32(float x)
 template <int CTRL>
 __device__ inline int dpp(int x)
 {
-    return __builtin_amdgcn_update_dpp(x, x, CTRL, 0xf, 0xf, false);
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true);   // every lane has a source: no old value
 }
 template <int CTRL>
 __device__ inline float dpp(float x)

@@ -7,9 +7,9 @@
 // four rotations without LDS, and the softmax's maximum and sum come of the same.
 //
 // The order is stable, so it needs every row's rank among the earlier rows of
-// its expert.  A workgroup ranks its own tokens' rows: one wave takes 64 rows at
-// a time, finds for each lane the lanes of the same expert by a ballot a bit of
-// the expert's number, and keeps the counts so far in LDS.  A second kernel sums
+// its expert.  A workgroup ranks its own tokens' rows: a wave takes 64 rows at a
+// time, finds for each lane the lanes of the same expert by a ballot a bit of the
+// expert's number, and keeps its counts so far in LDS.  A second kernel sums
 // the workgroups' counts over the workgroups, a third adds the experts' offsets
 // and writes both directions of the order.  Up to 64 tokens one workgroup does
 // all of it in one launch, which is what a decoding step waits for.
@@ -19,7 +19,8 @@ namespace hapmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPass = kThreads / 16;   // tokens of a workgroup at a time
+constexpr int kChoose = 512;           // threads of the first kernel
+constexpr int kPass = kThreads / 16;   // tokens of a workgroup of the gradient
 constexpr int kOneLaunch = 64;         // tokens
 constexpr int kPlaceRows = 1024;       // rows of a workgroup of the last kernel
 
@@ -50,8 +51,25 @@ __device__ inline void load_logits(float *v, const T *__restrict__ row, int lane
     for (int c = 0; c < PER; ++c) v[c] = keep && v[c] > -INFINITY ? v[c] : -INFINITY;
 }
 
-// exp(x - top), 1 where x is the largest: also where both are infinite
-__device__ inline float exp_from(float x, float top) { return x == top ? 1.0f : expf(x - top); }
+// exp(x - top), 1 where x is the largest: also where both are infinite.  2^t with t = x log2(e) in two parts, so that the
+// error is that of the instruction (one unit) and not t's rounding; 0 below 2^-126.
+__device__ inline float exp_from(float x, float top)
+{
+    const float d = fmaxf(x - top, -200.0f);
+    const float t = d * 1.44269504f, rest = __builtin_fmaf(d, 1.44269504f, -t) + d * 1.92596303e-8f;
+    const float y = __builtin_amdgcn_exp2f(t);
+    return x == top ? 1.0f : __builtin_fmaf(y, rest * 0.693147181f, y);
+}
+
+// Logits as whole numbers of the same order (both zeros equal), kClosed below all of them: the maxima need no care for
+// NaN, and the lane rotations go into them.
+constexpr int kClosed = INT32_MIN;
+__device__ inline int key_of(float x)
+{
+    const int b = __builtin_bit_cast(int, x + 0.0f);
+    return x == -INFINITY ? kClosed : b ^ (b >> 31 & 0x7fffffff);
+}
+__device__ inline float logit_of(int key) { return __builtin_bit_cast(float, key ^ (key >> 31 & 0x7fffffff)); }
 
 template <int PER>
 __device__ inline float softmax_sum(const float *v, float top)
@@ -62,12 +80,12 @@ __device__ inline float softmax_sum(const float *v, float top)
     return row_reduce(s, Sum());
 }
 
-template <int PER>
-__device__ inline float largest(const float *v)
+template <typename V, int PER>
+__device__ inline V largest(const V *v)
 {
-    float m = v[0];
+    V m = v[0];
 #pragma unroll
-    for (int c = 1; c < PER; ++c) m = fmaxf(m, v[c]);
+    for (int c = 1; c < PER; ++c) m = Max()(m, v[c]);
     return row_reduce(m, Max());
 }
 
@@ -83,9 +101,10 @@ __device__ inline uint64_t same_key(int key, int bits)
 }
 
 // Exclusive sums over count[0 .. experts) by the workgroup, in place; returns the total.  sh: one int a wave.
+template <int THREADS>
 __device__ inline int scan_counts(int *count, int experts, int *sh)
 {
-    constexpr int kPer = HAPMOE_MAX_EXPERTS / kThreads;
+    constexpr int kPer = HAPMOE_MAX_EXPERTS / THREADS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int own[kPer], sum = 0;
 #pragma unroll
@@ -104,7 +123,7 @@ __device__ inline int scan_counts(int *count, int experts, int *sh)
     __syncthreads();
     int before = inc - sum, total = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         before += w < wave ? sh[w] : 0;
         total += sh[w];
     }
@@ -121,123 +140,147 @@ __device__ inline int scan_counts(int *count, int experts, int *sh)
 // Choices, weights and ranks.  ALONE: the only workgroup, which finishes the order too; else rank goes to `place` and
 // the workgroup's counts to hist[workgroup][experts].
 template <typename T, int PER, bool VEC, bool ALONE>
-__global__ __launch_bounds__(kThreads) void k_choose(const T *__restrict__ logits, int64_t stride, int64_t tokens,
+__global__ __launch_bounds__(kChoose) void k_choose(const T *__restrict__ logits, int64_t stride, int64_t tokens,
                                                      int experts, int top_k, const uint8_t *__restrict__ keep,
                                                      int renormalize, int group, int bits, float *__restrict__ weight,
                                                      int32_t *__restrict__ expert, int32_t *__restrict__ place,
                                                      int32_t *__restrict__ hist, int32_t *__restrict__ count,
                                                      int32_t *__restrict__ offset, int32_t *__restrict__ slot)
 {
+    constexpr int kWaves = kChoose / 64;
     extern __shared__ int lds[];
-    int *sums = lds;                              // [experts]
-    int *chosen = lds + HAPMOE_MAX_EXPERTS;       // [group * top_k]
-    __shared__ int sh[kThreads / 64];
+    int *sums = lds;                         // [kWaves][experts]
+    int *chosen = lds + kWaves * experts;    // [group * top_k]
+    __shared__ int sh[kWaves];
     const int lane = threadIdx.x & 15;
     const int64_t first = (int64_t)blockIdx.x * group;
     const int here = tokens - first < group ? (int)(tokens - first) : group;
-    for (int e = threadIdx.x; e < experts; e += kThreads) sums[e] = 0;
-    for (int t0 = threadIdx.x >> 4; t0 < here; t0 += kPass) {
+    for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
+    for (int t0 = threadIdx.x >> 4; t0 < here; t0 += kChoose / 16) {
         const int64_t t = first + t0;
-        float v[PER];
-        load_logits<T, PER, VEC>(v, logits + t * stride, lane, experts, !keep || keep[t]);
-        const float top = largest<PER>(v);
-        float total = renormalize || top == -INFINITY ? 0.0f : softmax_sum<PER>(v, top);
-        float won[2] = {-INFINITY, -INFINITY};   // choices lane and lane + 16
+        float x[PER];
+        int v[PER];
+        load_logits<T, PER, VEC>(x, logits + t * stride, lane, experts, !keep || keep[t]);
+#pragma unroll
+        for (int c = 0; c < PER; ++c) v[c] = key_of(x[c]);
+        int m = largest<int, PER>(v);
+        const float top = logit_of(m);
+        float total = renormalize || m == kClosed ? 0.0f : softmax_sum<PER>(x, top);
+        int won[2] = {kClosed, kClosed};   // choices lane and lane + 16
         int who[2] = {-1, -1};
-        float m = top;
-        for (int j = 0; j < top_k && m > -INFINITY; ++j) {
+        for (int j = 0; j < top_k && m != kClosed; ++j) {
             int at = PER;
 #pragma unroll
             for (int c = PER - 1; c >= 0; --c) at = v[c] == m ? c : at;
             const int best = row_reduce(at < PER ? lane * PER + at : INT32_MAX, Min());
+            const int mine = best - lane * PER;
 #pragma unroll
-            for (int c = 0; c < PER; ++c) v[c] = lane * PER + c == best ? -INFINITY : v[c];
-            if (renormalize) total += exp_from(m, top);
+            for (int c = 0; c < PER; ++c) v[c] = c == mine ? kClosed : v[c];
+            if (renormalize) total += exp_from(logit_of(m), top);
             if (lane == (j & 15)) {
                 won[0] = j < 16 ? m : won[0];
                 who[0] = j < 16 ? best : who[0];
                 won[1] = j < 16 ? won[1] : m;
                 who[1] = j < 16 ? who[1] : best;
             }
-            m = largest<PER>(v);
+            m = largest<int, PER>(v);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int j = lane + 16 * h;
             if (j < top_k) {
-                weight[t * top_k + j] = who[h] < 0 ? 0.0f : exp_from(won[h], top) / total;
+                weight[t * top_k + j] = who[h] < 0 ? 0.0f : exp_from(logit_of(won[h]), top) / total;
                 expert[t * top_k + j] = who[h];
                 chosen[t0 * top_k + j] = who[h];
             }
         }
     }
     __syncthreads();
-    const int rows = here * top_k;
+    // each wave ranks a run of the rows among its own
+    const int rows = here * top_k, run = (rows + kChoose - 1) / kChoose * 64;
+    const int wave = threadIdx.x >> 6, wave_lane = threadIdx.x & 63;
+    const int lo = min(wave * run, rows), hi = min(lo + run, rows);
+    int *const own = sums + wave * experts;
     int32_t *const mine = place + first * top_k;
-    if (threadIdx.x < 64) {
-        for (int r0 = 0; r0 < rows; r0 += 64) {
-            const int r = r0 + (int)threadIdx.x;
-            const int e = r < rows ? chosen[r] : -1;
-            const uint64_t same = same_key(e + 1, bits);
-            const uint64_t below = same & ((1ull << threadIdx.x) - 1);
-            if (e >= 0) {
-                const int rank = sums[e] + __popcll(below);
-                if constexpr (ALONE)
-                    chosen[r] = rank << 10 | e;   // rank < 2^11, e < 2^10
-                else
-                    mine[r] = rank;
-            }
-            // the counts before this round are read by every lane before the lowest of each expert adds to them
-            __builtin_amdgcn_wave_barrier();
-            if (e >= 0 && below == 0) sums[e] += __popcll(same);
-            __builtin_amdgcn_wave_barrier();
-        }
+    for (int r0 = lo; r0 < hi; r0 += 64) {
+        const int r = r0 + wave_lane;
+        const int e = r < hi ? chosen[r] : -1;
+        const uint64_t same = same_key(e + 1, bits);
+        const uint64_t below = same & ((1ull << wave_lane) - 1);
+        if (e >= 0) chosen[r] = (own[e] + __popcll(below)) << 10 | e;   // rank < 2^11, e < 2^10
+        // the counts before this round are read by every lane before the lowest of each expert adds to them
+        __builtin_amdgcn_wave_barrier();
+        if (e >= 0 && below == 0) own[e] += __popcll(same);
+        __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
-    if constexpr (!ALONE) {
-        for (int e = threadIdx.x; e < experts; e += kThreads) hist[(int64_t)blockIdx.x * experts + e] = sums[e];
-    } else {
-        for (int e = threadIdx.x; e < experts; e += kThreads) count[e] = sums[e];
-        const int total = scan_counts(sums, experts, sh);
-        for (int e = threadIdx.x; e < experts; e += kThreads) offset[e] = sums[e];
+    // the counts of the waves before, and the whole
+    for (int e = threadIdx.x; e < experts; e += kChoose) {
+        int before = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const int n = sums[w * experts + e];
+            sums[w * experts + e] = before;
+            before += n;
+        }
+        if constexpr (ALONE)
+            count[e] = before;
+        else
+            hist[(int64_t)blockIdx.x * experts + e] = before;
+    }
+    __syncthreads();
+    if constexpr (ALONE) {
+        // experts' offsets into the last wave's place, then the others' by them
+        int *const at = chosen + rows;
+        for (int e = threadIdx.x; e < experts; e += kChoose) at[e] = count[e];
+        __syncthreads();
+        const int total = scan_counts<kChoose>(at, experts, sh);
+        for (int e = threadIdx.x; e < experts; e += kChoose) offset[e] = at[e];
         if (threadIdx.x == 0) offset[experts] = total;
-        for (int r = threadIdx.x; r < rows; r += kThreads) {
-            const int c = chosen[r];
-            const int p = c < 0 ? -1 : sums[c & 1023] + (c >> 10);
+        for (int r = threadIdx.x; r < rows; r += kChoose) {
+            const int c = chosen[r], e = c & 1023;
+            const int p = c < 0 ? -1 : at[e] + sums[r / run * experts + e] + (c >> 10);
             place[r] = p;
             if (p >= 0) slot[p] = r;
             if (r >= total) slot[r] = -1;
         }
+    } else {
+        for (int r = threadIdx.x; r < rows; r += kChoose) {
+            const int c = chosen[r];
+            mine[r] = c < 0 ? -1 : sums[r / run * experts + (c & 1023)] + (c >> 10);
+        }
     }
 }
 
-// hist[group][experts] -> the sums over the groups before, and count.  A workgroup takes 64 experts, wave w an equal
-// run of the groups: its sum, the waves' sums before it, then the running sum.
-constexpr int kScanWaves = 16;
-__global__ __launch_bounds__(64 * kScanWaves) void k_scan_groups(int32_t *__restrict__ hist, int groups, int experts,
-                                                                 int32_t *__restrict__ count)
+// hist[group][experts] -> the sums over the groups before, and count.  A workgroup takes 16 experts, 16 lanes an equal
+// run of the groups: its sum, the runs' sums before it, then the running sum.
+constexpr int kScanThreads = 1024, kRuns = kScanThreads / 16;
+__global__ __launch_bounds__(kScanThreads) void k_scan_groups(int32_t *__restrict__ hist, int groups, int experts,
+                                                              int32_t *__restrict__ count)
 {
-    __shared__ int part[kScanWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int e = blockIdx.x * 64 + lane;
-    const int run = (groups + kScanWaves - 1) / kScanWaves;
-    const int lo = wave * run < groups ? wave * run : groups, hi = lo + run < groups ? lo + run : groups;
+    __shared__ int part[kRuns][16];
+    const int lane = threadIdx.x & 15, run = threadIdx.x >> 4;
+    const int e = blockIdx.x * 16 + lane;
+    const int each = (groups + kRuns - 1) / kRuns;
+    const int lo = min(run * each, groups), hi = min(lo + each, groups);
     int sum = 0;
     if (e < experts) {
-#pragma unroll 16
+#pragma unroll 8
         for (int g = lo; g < hi; ++g) sum += hist[(int64_t)g * experts + e];
     }
-    part[wave][lane] = sum;
+    part[run][lane] = sum;
     __syncthreads();
-    int before = 0, total = 0;
 #pragma unroll
-    for (int w = 0; w < kScanWaves; ++w) {
-        before += w < wave ? part[w][lane] : 0;
-        total += part[w][lane];
+    for (int d = 1; d < kRuns; d <<= 1) {
+        const int o = run >= d ? part[run - d][lane] : 0;
+        __syncthreads();
+        part[run][lane] += o;
+        __syncthreads();
     }
     if (e >= experts) return;
-    if (wave == 0) count[e] = total;
-#pragma unroll 16
+    int before = part[run][lane] - sum;
+    if (run == kRuns - 1) count[e] = before + sum;
+#pragma unroll 8
     for (int g = lo; g < hi; ++g) {
         const int64_t i = (int64_t)g * experts + e;
         const int h = hist[i];
@@ -257,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void k_place(const int32_t *__restrict__ 
     __shared__ int sh[kThreads / 64];
     for (int e = threadIdx.x; e < experts; e += kThreads) at[e] = count[e];
     __syncthreads();
-    const int total = scan_counts(at, experts, sh);
+    const int total = scan_counts<kThreads>(at, experts, sh);
     if (blockIdx.x == 0) {
         for (int e = threadIdx.x; e < experts; e += kThreads) offset[e] = at[e];
         if (threadIdx.x == 0) offset[experts] = total;
@@ -286,9 +329,14 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
     const uint8_t *__restrict__ keep, int renormalize, const int32_t *__restrict__ expert,
     const float *__restrict__ weight, const float *__restrict__ d_weight, T *__restrict__ d_logits)
 {
+    // what the chosen add, [token][16 lanes' PER + 1]: a lane's are a row of their own, a row's banks shifted by one
+    __shared__ float added[kPass * 16 * (PER + 1)];
     const int lane = threadIdx.x & 15;
     const int64_t t = (int64_t)blockIdx.x * kPass + (threadIdx.x >> 4);
     if (t >= tokens) return;
+    float *const mine = added + threadIdx.x * (PER + 1), *const row = added + (threadIdx.x & ~15u) * (PER + 1);
+#pragma unroll
+    for (int c = 0; c < PER; ++c) mine[c] = 0.0f;
     int who[2];
     float gw[2], g[2], w[2];
 #pragma unroll
@@ -306,21 +354,19 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
         for (int c = 0; c < PER; ++c) d[c] = 0.0f;
     } else {
         load_logits<T, PER, VEC>(d, logits + t * stride, lane, experts, !keep || keep[t]);
-        const float top = largest<PER>(d);
+        const float top = largest<float, PER>(d);
         const float total = top == -INFINITY ? 1.0f : softmax_sum<PER>(d, top);
 #pragma unroll
         for (int c = 0; c < PER; ++c) d[c] = d[c] == -INFINITY ? 0.0f : exp_from(d[c], top) / total * -mean;
     }
-    const int row = threadIdx.x & 48;   // first lane of the row within the wave
-    for (int j = 0; j < top_k; ++j) {
-        const int h = j >> 4;
-        const int e = __shfl(h ? who[1] : who[0], row + (j & 15), 64);
-        const float add = __shfl(h ? w[1] * (renormalize ? g[1] - mean : g[1])
-                                   : w[0] * (renormalize ? g[0] - mean : g[0]),
-                                 row + (j & 15), 64);
+    // a token's choices are 16 lanes of one wave, and all different
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int c = 0; c < PER; ++c) d[c] += lane * PER + c == e ? add : 0.0f;
-    }
+    for (int h = 0; h < 2; ++h)
+        if (who[h] >= 0 && who[h] < 16 * PER) row[who[h] / PER * (PER + 1) + who[h] % PER] = w[h] * (renormalize ? g[h] - mean : g[h]);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int c = 0; c < PER; ++c) d[c] += mine[c];
     T *out = d_logits + t * experts + lane * PER;
     if constexpr (VEC) {
         constexpr int kStep = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER;
@@ -379,7 +425,7 @@ hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t to
     int bits = 1;
     while ((1 << bits) <= experts) ++bits;   // of the keys 0 .. experts
     const int rows_here = (int)(tokens < group ? tokens : group) * top_k;
-    const size_t lds = (HAPMOE_MAX_EXPERTS + (size_t)rows_here) * 4;
+    const size_t lds = ((kChoose / 64 + (alone ? 1 : 0)) * (size_t)experts + rows_here) * 4;
     hipError_t e = by_type(type, [&](auto t) {
         using T = decltype(t);
         return by_experts(experts, [&](auto per) {
@@ -387,14 +433,14 @@ hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t to
             const bool vec = experts == 16 * PER && aligned(logits, 16) && stride * (int64_t)sizeof(T) % 16 == 0;
             auto *kernel = alone ? (vec ? k_choose<T, PER, true, true> : k_choose<T, PER, false, true>)
                                  : (vec ? k_choose<T, PER, true, false> : k_choose<T, PER, false, false>);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), lds, s, static_cast<const T *>(logits),
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kChoose), lds, s, static_cast<const T *>(logits),
                                stride, tokens, experts, top_k, keep, renormalize ? 1 : 0, group, bits, weight, expert,
                                place, hist, count, offset, slot);
             return hipGetLastError();
         });
     });
     if (e != hipSuccess || alone) return e;
-    hipLaunchKernelGGL(k_scan_groups, dim3((unsigned)ceil_div(experts, 64)), dim3(64 * kScanWaves), 0, s, hist,
+    hipLaunchKernelGGL(k_scan_groups, dim3((unsigned)ceil_div(experts, 16)), dim3(kScanThreads), 0, s, hist,
                        (int)groups, experts, count);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int64_t rows = tokens * top_k;
