@@ -56,6 +56,20 @@ struct alignas(sizeof(T) * 8) Vec8 {
     T v[8];
 };
 
+// Such a vector that nothing reads again soon: kept out of the caches' way.
+template <typename T>
+__device__ inline Vec8<T> load_once(const T *p)
+{
+    typedef uint32_t W __attribute__((ext_vector_type(2 * sizeof(T))));
+    return __builtin_bit_cast(Vec8<T>, __builtin_nontemporal_load(reinterpret_cast<const W *>(p)));
+}
+template <typename T>
+__device__ inline void store_once(T *p, const Vec8<T> &v)
+{
+    typedef uint32_t W __attribute__((ext_vector_type(2 * sizeof(T))));
+    __builtin_nontemporal_store(__builtin_bit_cast(W, v), reinterpret_cast<W *>(p));
+}
+
 __device__ inline float to_f32(float x) { return x; }
 __device__ inline float to_f32(bf16 x) { return (float)x; }
 __device__ inline float to_f32(f16 x) { return (float)x; }
