@@ -519,7 +519,8 @@ int32_t hapmoe_route_backward(const void *d_logits, int32_t type, int64_t stride
 
 /* out[t] = sum_j weight[t][j] y[place[t][j]] for y [rows][hidden]: the outputs
  * of a token's experts put together, added in the order of j.  d_weight NULL:
- * weights 1 (with place of hapmoe_route the gradient of the rows' copying). */
+ * weights 1 (with place of hapmoe_route the gradient of the rows' copying).
+ * hidden <= 2^24. */
 int32_t hapmoe_combine(const void *d_y, int32_t type, int64_t rows, int64_t tokens, int32_t top_k, int64_t hidden,
                        const int32_t *d_place, const float *d_weight, void *d_out, void *stream);
 

@@ -243,13 +243,14 @@ __device__ inline int expert_of_rank(const int32_t *offset, int experts, int64_t
 }
 
 // The tile of a workgroup of d_w: the experts by falling number of rows, each one's tiles spread over the XCDs.  False for
-// one past an expert's tiles.
+// one past an expert's tiles or past the last expert.
 __device__ inline bool find_grad_w_tile(const int32_t *offset, int experts, int64_t rows, int p_tiles, int q_tiles,
                                         uint32_t block, Tile &t)
 {
     const uint32_t tiles = (uint32_t)p_tiles * q_tiles, rounds = (tiles + 7) & ~7u;
     const int id = (int)xcd_order(block % rounds, tiles);
     if (id < 0) return false;
+    if (block / rounds >= (uint32_t)experts) return false;
     t.expert = expert_of_rank(offset, experts, rows, (int)(block / rounds));
     t.q = id % q_tiles;
     t.p = id / q_tiles;
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_product(const ExpertProduct a, 
     int64_t q_end, p_end, out_row;
     int k_end;
     if constexpr (KIND == kGradW) {
-        if (!find_grad_w_tile(a.offset, a.experts, a.rows, p_tiles, q_tiles, blockIdx.x, t)) return;
+        if (!find_grad_w_tile(a.offset, a.experts, a.rows, p_tiles, q_tiles, (uint32_t)workgroup(), t)) return;
         q_end = a.outputs;
         p_end = a.inputs;
         k_end = t.hi - t.lo;
@@ -427,7 +428,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_product(const ExpertProduct a, 
         }
         if (GATHER && a.x_rows == 0) k_end = 0;
     } else {
-        if (!find_tile<B>(a.offset, a.experts, a.rows, p_tiles, blockIdx.x, t)) return;
+        if (!find_tile<B>(a.offset, a.experts, a.rows, p_tiles, workgroup(), t)) return;
         q_end = t.hi - t.lo;
         p_end = KIND == kForward ? a.outputs : a.inputs;
         k_end = t.expert == a.experts ? 0 : KIND == kForward ? (int)a.inputs : (int)a.outputs;
@@ -492,7 +493,7 @@ hipError_t launch(const ExpertProduct &a, hipStream_t s)
                                          : most_row_tiles(a.rows, a.experts, B) * p_tiles;
     const int64_t grid = ceil_div(tiles, 8) * 8;   // whole rounds of the XCDs
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_product<KIND, T, O, GATHER, SMALL, B, AHEAD>), dim3((unsigned)grid), dim3(kThreads), 0, s, a,
+    hipLaunchKernelGGL((k_product<KIND, T, O, GATHER, SMALL, B, AHEAD>), many(grid), dim3(kThreads), 0, s, a,
                        (int)p_tiles, (int)q_tiles);
     return hipGetLastError();
 }
@@ -733,7 +734,7 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
     int64_t q_end, p_end, out_row;
     int k_end;
     if constexpr (KIND == kGradW) {
-        if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, blockIdx.x, t)) return;
+        if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, (uint32_t)workgroup(), t)) return;
         q_end = a.outputs;
         p_end = a.inputs;
         k_end = t.hi - t.lo;
@@ -743,7 +744,7 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
             lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, t.lo, a.x_rows, (int64_t)t.p * BP, p_end, k_end);
         }
     } else {
-        if (!find_tile<BQ>(a.offset, a.experts, a.rows, args.p_tiles, blockIdx.x, t)) return;
+        if (!find_tile<BQ>(a.offset, a.experts, a.rows, args.p_tiles, workgroup(), t)) return;
         q_end = t.hi - t.lo;
         p_end = KIND == kForward ? a.outputs : a.inputs;
         k_end = t.expert == a.experts ? 0 : KIND == kForward ? (int)a.inputs : (int)a.outputs;
@@ -889,7 +890,7 @@ __global__ __launch_bounds__(256, 2) void k_grad_w(const Args args)
     __shared__ u32x4 lds[kStages * (kTileQ + kTileP)];
     const ExpertProduct &a = args.a;
     Tile t;
-    if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, blockIdx.x, t)) return;
+    if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, (uint32_t)workgroup(), t)) return;
     const int64_t q0 = (int64_t)t.q * BQ, p0 = (int64_t)t.p * BP;
     const int k_end = t.hi - t.lo;
     Loader<false, BQ, kThreads, false, kDepth> lq;
@@ -983,10 +984,10 @@ hipError_t launch(const ExpertProduct &a, hipStream_t s)
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
     constexpr int kThreads = 64 * WQ * WP;
     if (a.slot && KIND != kGradX)
-        hipLaunchKernelGGL((k_product<KIND, T, O, true, BQ, BP, WQ, WP, STAGES>), dim3((unsigned)grid), dim3(kThreads),
+        hipLaunchKernelGGL((k_product<KIND, T, O, true, BQ, BP, WQ, WP, STAGES>), many(grid), dim3(kThreads),
                            0, s, args);
     else
-        hipLaunchKernelGGL((k_product<KIND, T, O, false, BQ, BP, WQ, WP, STAGES>), dim3((unsigned)grid),
+        hipLaunchKernelGGL((k_product<KIND, T, O, false, BQ, BP, WQ, WP, STAGES>), many(grid),
                            dim3(kThreads), 0, s, args);
     return hipGetLastError();
 }
@@ -1001,7 +1002,7 @@ hipError_t launch_grad_w(const ExpertProduct &a, hipStream_t s)
     args.q_tiles = (int)ceil_div(a.outputs, BQ);
     const int64_t grid = grad_w_grid(a.experts, args.p_tiles, args.q_tiles);
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((a.slot ? k_grad_w<T, O, true, BQ, BP> : k_grad_w<T, O, false, BQ, BP>), dim3((unsigned)grid),
+    hipLaunchKernelGGL((a.slot ? k_grad_w<T, O, true, BQ, BP> : k_grad_w<T, O, false, BQ, BP>), many(grid),
                        dim3(256), 0, s, args);
     return hipGetLastError();
 }

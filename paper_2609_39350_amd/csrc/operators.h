@@ -16,6 +16,17 @@ inline int64_t type_bytes(int type) { return type == HAPMOE_F32 ? 4 : 2; }
 inline bool aligned(const void *p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+#ifdef __HIPCC__
+// A launch's threads along one axis have to stay below 2^32, so many workgroups take two axes, here x and z; those of
+// the last z that exceed n are the kernel's to leave out.
+inline dim3 many(int64_t n, unsigned y = 1)
+{
+    constexpr int64_t kMost = int64_t(1) << 22;   // of up to 1,024 threads
+    return n <= kMost ? dim3((unsigned)n, y) : dim3((unsigned)kMost, y, (unsigned)ceil_div(n, kMost));
+}
+__device__ inline int64_t workgroup() { return (int64_t)blockIdx.z * gridDim.x + blockIdx.x; }
+#endif
+
 hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t tokens, int experts, int top_k,
                         const uint8_t *keep, bool renormalize, float *weight, int32_t *expert, int32_t *count,
                         int32_t *offset, int32_t *slot, int32_t *place, void *ws, hipStream_t s);

@@ -153,7 +153,8 @@ __global__ __launch_bounds__(kChoose) void k_choose(const T *__restrict__ logits
     int *chosen = lds + kWaves * experts;    // [group * top_k]
     __shared__ int sh[kWaves];
     const int lane = threadIdx.x & 15;
-    const int64_t first = (int64_t)blockIdx.x * group;
+    const int64_t first = workgroup() * group;
+    if (first >= tokens && first > 0) return;
     const int here = tokens - first < group ? (int)(tokens - first) : group;
     for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
     for (int t0 = threadIdx.x >> 4; t0 < here; t0 += kChoose / 16) {
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(kChoose) void k_choose(const T *__restrict__ logits
         if constexpr (ALONE)
             count[e] = before;
         else
-            hist[(int64_t)blockIdx.x * experts + e] = before;
+            hist[workgroup() * experts + e] = before;
     }
     __syncthreads();
     if constexpr (ALONE) {
@@ -301,11 +302,11 @@ __global__ __launch_bounds__(kThreads) void k_place(const int32_t *__restrict__ 
     for (int e = threadIdx.x; e < experts; e += kThreads) at[e] = count[e];
     __syncthreads();
     const int total = scan_counts<kThreads>(at, experts, sh);
-    if (blockIdx.x == 0) {
+    if (workgroup() == 0) {
         for (int e = threadIdx.x; e < experts; e += kThreads) offset[e] = at[e];
         if (threadIdx.x == 0) offset[experts] = total;
     }
-    const int64_t r0 = (int64_t)blockIdx.x * kPlaceRows;
+    const int64_t r0 = workgroup() * kPlaceRows;
 #pragma unroll
     for (int i = 0; i < kPlaceRows / kThreads; ++i) {
         const int64_t r = r0 + i * kThreads + threadIdx.x;
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
     // what the chosen add, [token][16 lanes' PER + 1]: a lane's are a row of their own, a row's banks shifted by one
     __shared__ float added[kPass * 16 * (PER + 1)];
     const int lane = threadIdx.x & 15;
-    const int64_t t = (int64_t)blockIdx.x * kPass + (threadIdx.x >> 4);
+    const int64_t t = workgroup() * kPass + (threadIdx.x >> 4);
     if (t >= tokens) return;
     float *const mine = added + threadIdx.x * (PER + 1), *const row = added + (threadIdx.x & ~15u) * (PER + 1);
 #pragma unroll
@@ -433,7 +434,7 @@ hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t to
             const bool vec = experts == 16 * PER && aligned(logits, 16) && stride * (int64_t)sizeof(T) % 16 == 0;
             auto *kernel = alone ? (vec ? k_choose<T, PER, true, true> : k_choose<T, PER, false, true>)
                                  : (vec ? k_choose<T, PER, true, false> : k_choose<T, PER, false, false>);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kChoose), lds, s, static_cast<const T *>(logits),
+            hipLaunchKernelGGL(kernel, many(groups), dim3(kChoose), lds, s, static_cast<const T *>(logits),
                                stride, tokens, experts, top_k, keep, renormalize ? 1 : 0, group, bits, weight, expert,
                                place, hist, count, offset, slot);
             return hipGetLastError();
@@ -444,7 +445,7 @@ hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t to
                        (int)groups, experts, count);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int64_t rows = tokens * top_k;
-    hipLaunchKernelGGL(k_place, dim3((unsigned)ceil_div(rows, kPlaceRows)), dim3(kThreads), 0, s, expert, hist, count,
+    hipLaunchKernelGGL(k_place, many(ceil_div(rows, kPlaceRows)), dim3(kThreads), 0, s, expert, hist, count,
                        rows, experts, group * top_k, offset, place, slot);
     return hipGetLastError();
 }
@@ -460,7 +461,7 @@ hipError_t launch_route_backward(const void *logits, int type, int64_t stride, i
             const bool vec = experts == 16 * PER && aligned(logits, 16) && aligned(d_logits, 16) &&
                              stride * (int64_t)sizeof(T) % 16 == 0;
             hipLaunchKernelGGL((vec ? k_route_backward<T, PER, true> : k_route_backward<T, PER, false>),
-                               dim3((unsigned)ceil_div(tokens, kPass)), dim3(kThreads), 0, s,
+                               many(ceil_div(tokens, kPass)), dim3(kThreads), 0, s,
                                static_cast<const T *>(logits), stride, tokens, experts, top_k, keep,
                                renormalize ? 1 : 0, expert, weight, d_weight, static_cast<T *>(d_logits));
             return hipGetLastError();

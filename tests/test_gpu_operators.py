@@ -733,3 +733,57 @@ def test_refusals():
                 {"lr": 1e-3, "step": 1, "eps": math.nan}):
         with pytest.raises(ops.binding.HapmoeError):
             opt.step(p, **bad)
+
+
+# ------------------------------------------------- more workgroups than one axis of a launch holds
+def test_route_past_one_axis_of_workgroups():
+    """2^28 tokens: the gradient takes 2^24 workgroups of 256 threads."""
+    T = (1 << 28) + 5
+    say("route", T)
+    logits = torch.zeros(T, 2, dtype=torch.bfloat16, device="cuda")
+    second = torch.arange(T, device="cuda") % 3 == 0
+    logits[:, 1] = torch.where(second, 1.0, -1.0)
+    r = ops.route(logits, 1, renormalize=False)
+    assert torch.equal(r.expert[:, 0] == 1, second)
+    n = int(second.sum())
+    assert r.count.tolist() == [T - n, n] and r.offset.tolist() == [0, T - n, T]
+    assert torch.equal(torch.sort(r.place[:, 0][second]).values, torch.arange(T - n, T, device="cuda", dtype=torch.int32))
+    assert torch.equal(r.slot[r.place[:, 0].long()], torch.arange(T, device="cuda", dtype=torch.int32))
+    d = ops.route_backward(logits, r, torch.ones_like(r.weight), renormalize=False)
+    p = 1 / (1 + math.exp(-1.0))
+    unit = p * (1 - p) * 2.0 ** -8
+    del logits
+    for e in (0, 1):
+        want = torch.where(second == (e == 1), p * (1 - p), -p * (1 - p))
+        assert (d[:, e].float() - want.float()).abs().max() <= 2 * unit
+
+
+@pytest.mark.parametrize("hidden", [3, 8])
+def test_combine_past_one_axis_of_workgroups(hidden):
+    """2^24 tokens are 2^24 workgroups of 256 threads; of the gradient, 2^26 rows."""
+    T = (1 << 24) + 7
+    say("combine", T, hidden)
+    y = torch.arange(T, device="cuda").remainder(251).to(torch.bfloat16)[:, None].expand(T, hidden).contiguous()
+    place = torch.arange(T - 1, -1, -1, device="cuda", dtype=torch.int32)[:, None].contiguous()
+    assert torch.equal(ops.combine(y, place), y.flip(0))
+    T = (1 << 26) + 9
+    d_out = torch.arange(T, device="cuda").remainder(127).to(torch.bfloat16)[:, None].expand(T, hidden).contiguous()
+    y = torch.ones_like(d_out)
+    place = torch.arange(T - 1, -1, -1, device="cuda", dtype=torch.int32)
+    d_y, d_weight = ops.combine_backward(d_out, y, place, place[:, None].contiguous(),
+                                         torch.full((T, 1), 2.0, device="cuda"))
+    assert torch.equal(d_y, (d_out * 2).flip(0))
+    assert torch.equal(d_weight[:, 0], d_out[:, 0].float() * hidden)
+
+
+def test_products_past_one_axis_of_workgroups():
+    """2^30 rows of one column are 2^24 tiles of 64 rows."""
+    R = (1 << 30) + 100
+    say("products", R)
+    x = torch.arange(R, device="cuda", dtype=torch.int32).remainder(127).to(torch.bfloat16)[:, None]
+    w = torch.full((2, 1, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    w[1] = 0.5
+    cut = (1 << 30) - 5
+    off = torch.tensor([0, cut, R], dtype=torch.int32, device="cuda")
+    for y in (ops.expert_matmul(x, w, off), ops.expert_matmul_grad_x(x, w, off)):
+        assert torch.equal(y[:cut], x[:cut] * 2) and torch.equal(y[cut:], x[cut:] * 0.5)
