@@ -1,10 +1,11 @@
 // The router: of every token's logits the top_k largest, their softmax weights,
 // and the order that puts each expert's rows together; and its gradient.
 //
-// Sixteen lanes take a token (four tokens a wave): lane l holds the logits
-// l * PER .. l * PER + PER - 1 in registers, so a choice is two reductions over
-// a row of lanes (the largest logit, then the lowest index that has it), each
-// four rotations without LDS, and the softmax's maximum and sum come of the same.
+// Sixteen lanes take a token (four tokens a wave), its logits in their registers.
+// A choice is the largest key over a row of lanes, four rotations without LDS,
+// then the lowest index that has it; the softmax's maximum and sum come of the
+// same.  From 129 experts on the keys are in LDS too and a choice looks again
+// at the chosen lane's alone.
 //
 // The order is stable, so it needs every row's rank among the earlier rows of
 // its expert.  A workgroup ranks its own tokens' rows: a wave takes 64 rows at a
@@ -13,13 +14,16 @@
 // the workgroups' counts over the workgroups, a third adds the experts' offsets
 // and writes both directions of the order.  Up to 64 tokens one workgroup does
 // all of it in one launch, which is what a decoding step waits for.
+//
+// 32,768 tokens, 256 fp32 logits, top 8: choices 16.6 us (instruction issue; 7 of
+// them would be the reading; 21.4 with all keys in registers), the groups' sums 4.7,
+// the order 6.9, the gradient 12.4 (its 67 MB at 5.4 TB/s).  4 tokens of 64: 4.7 us.
 #include "operators.h"
 
 namespace hapmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChoose = 512;           // threads of the first kernel
 constexpr int kPass = kThreads / 16;   // tokens of a workgroup of the gradient
 constexpr int kOneLaunch = 64;         // tokens
 constexpr int kPlaceRows = 1024;       // rows of a workgroup of the last kernel
@@ -27,36 +31,56 @@ constexpr int kPlaceRows = 1024;       // rows of a workgroup of the last kernel
 // tokens of a workgroup
 __host__ __device__ inline int group_tokens(int64_t tokens) { return tokens <= 64 * 512 ? 32 : 64; }
 
+// Neighbouring elements of a lane: those that it loads and stores at once where vectors are aligned; where they are not
+// it has the same, so that sums have the same order.
+template <typename T, int PER>
+constexpr int kStep = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER;
+template <typename T, int N>
+struct alignas(N * sizeof(T)) Piece {
+    T x[N];
+};
+// The expert whose logit is a lane's c-th: lanes take turns at steps of a row, so that loads and stores are whole lines, or
+// each has a RUN of PER, for the lowest of equal logits.
+template <int STEP, int PER, bool RUN>
+__device__ inline int expert_at(int lane, int c)
+{
+    return RUN ? lane * PER + c : (c / STEP * 16 + lane) * STEP + c % STEP;
+}
+
 // A token's logits in the registers of 16 lanes; closed experts (-inf, NaN, past the end, keep = 0) are -inf.
-template <typename T, int PER, bool VEC>
+template <typename T, int PER, bool VEC, bool RUN>
 __device__ inline void load_logits(float *v, const T *__restrict__ row, int lane, int experts, bool keep)
 {
-    const int base = lane * PER;
-    if constexpr (VEC) {
-        constexpr int kStep = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER;
-        struct alignas(kStep * sizeof(T)) Piece {
-            T x[kStep];
-        };
+    constexpr int kN = kStep<T, PER>;
 #pragma unroll
-        for (int c = 0; c < PER; c += kStep) {
-            const Piece p = *reinterpret_cast<const Piece *>(row + base + c);
+    for (int c = 0; c < PER; c += kN) {
+        const int e = expert_at<kN, PER, RUN>(lane, c);
+        if constexpr (VEC) {
+            const auto p = *reinterpret_cast<const Piece<T, kN> *>(row + e);
 #pragma unroll
-            for (int i = 0; i < kStep; ++i) v[c + i] = to_f32(p.x[i]);
+            for (int i = 0; i < kN; ++i) v[c + i] = to_f32(p.x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) v[c + i] = e + i < experts ? to_f32(row[e + i]) : -INFINITY;
         }
-    } else {
-#pragma unroll
-        for (int c = 0; c < PER; ++c) v[c] = base + c < experts ? to_f32(row[base + c]) : -INFINITY;
     }
 #pragma unroll
     for (int c = 0; c < PER; ++c) v[c] = keep && v[c] > -INFINITY ? v[c] : -INFINITY;
 }
+
+// threads of the first kernel: 32 KB of keys where they are in LDS, so that four workgroups share a CU
+constexpr int choose_threads(int per) { return per <= 16 ? 512 : 8192 / per; }
+// Where a lane's keys are in LDS too.  Taking a choice out of registers costs every lane a look at all of its PER keys,
+// three times; out of LDS the 16 lanes look at the chosen lane's keys together, once.
+constexpr bool keys_in_lds(int per) { return per >= 16; }
+constexpr int key_row(int per) { return 16 * per + 16; }   // a token's keys, the tokens' banks shifted
 
 // exp(x - top), 1 where x is the largest: also where both are infinite.  2^t with t = x log2(e) in two parts, so that the
 // error is that of the instruction (one unit) and not t's rounding; 0 below 2^-126.
 __device__ inline float exp_from(float x, float top)
 {
     const float d = fmaxf(x - top, -200.0f);
-    const float t = d * 1.44269504f, rest = __builtin_fmaf(d, 1.44269504f, -t) + d * 1.92596303e-8f;
+    const float t = d * 1.44269504f, rest = __builtin_fmaf(d, 1.92596303e-8f, __builtin_fmaf(d, 1.44269504f, -t));
     const float y = __builtin_amdgcn_exp2f(t);
     return x == top ? 1.0f : __builtin_fmaf(y, rest * 0.693147181f, y);
 }
@@ -71,22 +95,36 @@ __device__ inline int key_of(float x)
 }
 __device__ inline float logit_of(int key) { return __builtin_bit_cast(float, key ^ (key >> 31 & 0x7fffffff)); }
 
+// v to exp(v - top), 0 where closed (top is not), and their sum
 template <int PER>
-__device__ inline float softmax_sum(const float *v, float top)
+__device__ inline float softmax(float *v, float top)
 {
     float s = 0.0f;
 #pragma unroll
-    for (int c = 0; c < PER; ++c) s += v[c] == -INFINITY ? 0.0f : exp_from(v[c], top);
+    for (int c = 0; c < PER; ++c) s += v[c] = exp_from(v[c], top);
     return row_reduce(s, Sum());
 }
 
 template <typename V, int PER>
-__device__ inline V largest(const V *v)
+__device__ inline V lane_largest(const V *v)
 {
     V m = v[0];
 #pragma unroll
     for (int c = 1; c < PER; ++c) m = Max()(m, v[c]);
-    return row_reduce(m, Max());
+    return m;
+}
+
+// The lowest lane of this lane's row of 16 where yes; 31 if none.
+__device__ inline int first_of_row(bool yes)
+{
+    return __ffs((int)((uint32_t)(__ballot(yes) >> (threadIdx.x & 48)) & 0xffff) | INT32_MIN) - 1;
+}
+
+// LDS written by lanes of a wave and read by others of it: its accesses are done in order, the compiler has to keep it.
+__device__ inline void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // For each lane the lanes of the wave whose `key` is the same; bits: of the keys.
@@ -140,61 +178,98 @@ __device__ inline int scan_counts(int *count, int experts, int *sh)
 // Choices, weights and ranks.  ALONE: the only workgroup, which finishes the order too; else rank goes to `place` and
 // the workgroup's counts to hist[workgroup][experts].
 template <typename T, int PER, bool VEC, bool ALONE>
-__global__ __launch_bounds__(kChoose) void k_choose(const T *__restrict__ logits, int64_t stride, int64_t tokens,
-                                                     int experts, int top_k, const uint8_t *__restrict__ keep,
-                                                     int renormalize, int group, int bits, float *__restrict__ weight,
-                                                     int32_t *__restrict__ expert, int32_t *__restrict__ place,
-                                                     int32_t *__restrict__ hist, int32_t *__restrict__ count,
-                                                     int32_t *__restrict__ offset, int32_t *__restrict__ slot)
+__global__ __launch_bounds__(choose_threads(PER)) void k_choose(
+    const T *__restrict__ logits, int64_t stride, int64_t tokens, int experts, int top_k,
+    const uint8_t *__restrict__ keep, int renormalize, int group, int bits, float *__restrict__ weight,
+    int32_t *__restrict__ expert, int32_t *__restrict__ place, int32_t *__restrict__ hist, int32_t *__restrict__ count,
+    int32_t *__restrict__ offset, int32_t *__restrict__ slot)
 {
-    constexpr int kWaves = kChoose / 64;
-    extern __shared__ int lds[];
-    int *sums = lds;                         // [kWaves][experts]
-    int *chosen = lds + kWaves * experts;    // [group * top_k]
-    __shared__ int sh[kWaves];
-    const int lane = threadIdx.x & 15;
+    constexpr int kChoose = choose_threads(PER), kWaves = kChoose / 64;
+    constexpr bool kInLds = keys_in_lds(PER);
+    extern __shared__ __attribute__((aligned(16))) int lds[];
     const int64_t first = workgroup() * group;
     if (first >= tokens && first > 0) return;
     const int here = tokens - first < group ? (int)(tokens - first) : group;
-    for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
+    int *const chosen = lds;                              // [here * top_k], whole vectors
+    int *const sums = lds + ((here * top_k + 3) & ~3);    // [kWaves][experts]; before that the tokens' keys
+    __shared__ int sh[kWaves];
+    const int lane = threadIdx.x & 15;
+    if constexpr (!kInLds)
+        for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
     for (int t0 = threadIdx.x >> 4; t0 < here; t0 += kChoose / 16) {
         const int64_t t = first + t0;
         float x[PER];
         int v[PER];
-        load_logits<T, PER, VEC>(x, logits + t * stride, lane, experts, !keep || keep[t]);
+        load_logits<T, PER, VEC, true>(x, logits + t * stride, lane, experts, !keep || keep[t]);
 #pragma unroll
         for (int c = 0; c < PER; ++c) v[c] = key_of(x[c]);
-        int m = largest<int, PER>(v);
+        int *const row = sums + (threadIdx.x >> 4) * key_row(PER);
+        if constexpr (kInLds) {
+            wave_order();   // the keys of the token before are read
+#pragma unroll
+            for (int c = 0; c < PER; c += 4)
+                *reinterpret_cast<int4 *>(row + lane * PER + c) = make_int4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+            wave_order();
+        }
+        int own = lane_largest<int, PER>(v);   // the largest of the lane's keys that are left
+        int m = row_reduce(own, Max());
         const float top = logit_of(m);
-        float total = renormalize || m == kClosed ? 0.0f : softmax_sum<PER>(x, top);
+        float total = renormalize || m == kClosed ? 0.0f : softmax<PER>(x, top);
         int won[2] = {kClosed, kClosed};   // choices lane and lane + 16
         int who[2] = {-1, -1};
         for (int j = 0; j < top_k && m != kClosed; ++j) {
-            int at = PER;
+            int best;
+            if constexpr (kInLds) {
+                const int from = first_of_row(own == m);
+                int k[PER / 16], at = 0;
 #pragma unroll
-            for (int c = PER - 1; c >= 0; --c) at = v[c] == m ? c : at;
-            const int best = row_reduce(at < PER ? lane * PER + at : INT32_MAX, Min());
-            const int mine = best - lane * PER;
+                for (int q = 0; q < PER / 16; ++q) k[q] = row[from * PER + 16 * q + lane];
 #pragma unroll
-            for (int c = 0; c < PER; ++c) v[c] = c == mine ? kClosed : v[c];
-            if (renormalize) total += exp_from(logit_of(m), top);
-            if (lane == (j & 15)) {
-                won[0] = j < 16 ? m : won[0];
-                who[0] = j < 16 ? best : who[0];
-                won[1] = j < 16 ? won[1] : m;
-                who[1] = j < 16 ? who[1] : best;
+                for (int q = PER / 16 - 1; q >= 0; --q) {
+                    const int l = first_of_row(k[q] == m);
+                    at = l < 16 ? 16 * q + l : at;
+                }
+                best = from * PER + at;
+#pragma unroll
+                for (int q = 0; q < PER / 16; ++q) k[q] = at == 16 * q + lane ? kClosed : k[q];
+                if (lane == 0) row[best] = kClosed;
+                wave_order();
+                const int left = row_reduce(lane_largest<int, PER / 16>(k), Max());
+                own = lane == from ? left : own;
+            } else {
+                int at = PER;
+#pragma unroll
+                for (int c = PER - 1; c >= 0; --c) at = v[c] == m ? c : at;
+                best = row_reduce(at < PER ? lane * PER + at : INT32_MAX, Min());
+                const int mine = best - lane * PER;
+#pragma unroll
+                for (int c = 0; c < PER; ++c) v[c] = c == mine ? kClosed : v[c];
+                own = lane_largest<int, PER>(v);
             }
-            m = largest<int, PER>(v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                won[h] = lane + 16 * h == j ? m : won[h];
+                who[h] = lane + 16 * h == j ? best : who[h];
+            }
+            m = row_reduce(own, Max());
         }
+        float share[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) share[h] = who[h] < 0 ? 0.0f : exp_from(logit_of(won[h]), top);
+        if (renormalize) total = row_reduce(share[0] + share[1], Sum());
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int j = lane + 16 * h;
             if (j < top_k) {
-                weight[t * top_k + j] = who[h] < 0 ? 0.0f : exp_from(logit_of(won[h]), top) / total;
+                weight[t * top_k + j] = who[h] < 0 ? 0.0f : share[h] / total;
                 expert[t * top_k + j] = who[h];
                 chosen[t0 * top_k + j] = who[h];
             }
         }
+    }
+    if constexpr (kInLds) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
     }
     __syncthreads();
     // each wave ranks a run of the rows among its own
@@ -210,9 +285,9 @@ __global__ __launch_bounds__(kChoose) void k_choose(const T *__restrict__ logits
         const uint64_t below = same & ((1ull << wave_lane) - 1);
         if (e >= 0) chosen[r] = (own[e] + __popcll(below)) << 10 | e;   // rank < 2^11, e < 2^10
         // the counts before this round are read by every lane before the lowest of each expert adds to them
-        __builtin_amdgcn_wave_barrier();
+        wave_order();
         if (e >= 0 && below == 0) own[e] += __popcll(same);
-        __builtin_amdgcn_wave_barrier();
+        wave_order();
     }
     __syncthreads();
     // the counts of the waves before, and the whole
@@ -231,8 +306,7 @@ __global__ __launch_bounds__(kChoose) void k_choose(const T *__restrict__ logits
     }
     __syncthreads();
     if constexpr (ALONE) {
-        // experts' offsets into the last wave's place, then the others' by them
-        int *const at = chosen + rows;
+        int *const at = sums + kWaves * experts;
         for (int e = threadIdx.x; e < experts; e += kChoose) at[e] = count[e];
         __syncthreads();
         const int total = scan_counts<kChoose>(at, experts, sh);
@@ -255,38 +329,47 @@ __global__ __launch_bounds__(kChoose) void k_choose(const T *__restrict__ logits
 
 // hist[group][experts] -> the sums over the groups before, and count.  A workgroup takes 16 experts, 16 lanes an equal
 // run of the groups: its sum, the runs' sums before it, then the running sum.
-constexpr int kScanThreads = 1024, kRuns = kScanThreads / 16;
+constexpr int kScanThreads = 1024, kScanExperts = 16, kRuns = kScanThreads / kScanExperts;
 __global__ __launch_bounds__(kScanThreads) void k_scan_groups(int32_t *__restrict__ hist, int groups, int experts,
                                                               int32_t *__restrict__ count)
 {
-    __shared__ int part[kRuns][16];
-    const int lane = threadIdx.x & 15, run = threadIdx.x >> 4;
-    const int e = blockIdx.x * 16 + lane;
+    constexpr int kKept = 16;   // counts in registers: a run that is no longer is loaded once
+    __shared__ int part[kScanThreads / 64][kScanExperts];
+    const int mine = threadIdx.x % kScanExperts, run = threadIdx.x / kScanExperts;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int e = blockIdx.x * kScanExperts + mine;
     const int each = (groups + kRuns - 1) / kRuns;
-    const int lo = min(run * each, groups), hi = min(lo + each, groups);
-    int sum = 0;
-    if (e < experts) {
-#pragma unroll 8
-        for (int g = lo; g < hi; ++g) sum += hist[(int64_t)g * experts + e];
-    }
-    part[run][lane] = sum;
-    __syncthreads();
+    const int lo = min(run * each, groups), hi = e < experts ? min(lo + each, groups) : lo;
+    int32_t *const own = hist + e;
+    int kept[kKept], sum = 0;
+    auto load = [&](int g0) {
 #pragma unroll
-    for (int d = 1; d < kRuns; d <<= 1) {
-        const int o = run >= d ? part[run - d][lane] : 0;
-        __syncthreads();
-        part[run][lane] += o;
-        __syncthreads();
+        for (int i = 0; i < kKept; ++i) kept[i] = g0 + i < hi ? own[(int64_t)(g0 + i) * experts] : 0;
+    };
+    for (int g = lo; g < hi; g += kKept) {
+        load(g);
+#pragma unroll
+        for (int i = 0; i < kKept; ++i) sum += kept[i];
     }
-    if (e >= experts) return;
-    int before = part[run][lane] - sum;
-    if (run == kRuns - 1) count[e] = before + sum;
-#pragma unroll 8
-    for (int g = lo; g < hi; ++g) {
-        const int64_t i = (int64_t)g * experts + e;
-        const int h = hist[i];
-        hist[i] = before;
-        before += h;
+    int before = sum;
+#pragma unroll
+    for (int d = kScanExperts; d < 64; d <<= 1) {
+        const int o = __shfl_up(before, d, 64);
+        before += lane >= d ? o : 0;
+    }
+    if (lane >= 64 - kScanExperts) part[wave][mine] = before;
+    __syncthreads();
+    before -= sum;
+#pragma unroll
+    for (int w = 0; w < kScanThreads / 64; ++w) before += w < wave ? part[w][mine] : 0;
+    if (e < experts && run == kRuns - 1) count[e] = before + sum;
+    for (int g = lo; g < hi; g += kKept) {
+        if (each > kKept) load(g);
+#pragma unroll
+        for (int i = 0; i < kKept; ++i) {
+            if (g + i < hi) own[(int64_t)(g + i) * experts] = before;
+            before += kept[i];
+        }
     }
 }
 
@@ -354,37 +437,36 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
 #pragma unroll
         for (int c = 0; c < PER; ++c) d[c] = 0.0f;
     } else {
-        load_logits<T, PER, VEC>(d, logits + t * stride, lane, experts, !keep || keep[t]);
-        const float top = largest<float, PER>(d);
-        const float total = top == -INFINITY ? 1.0f : softmax_sum<PER>(d, top);
+        load_logits<T, PER, VEC, false>(d, logits + t * stride, lane, experts, !keep || keep[t]);
+        const float top = row_reduce(lane_largest<float, PER>(d), Max());
+        const float total = top == -INFINITY ? 1.0f : softmax<PER>(d, top), scale = -mean / total;
 #pragma unroll
-        for (int c = 0; c < PER; ++c) d[c] = d[c] == -INFINITY ? 0.0f : exp_from(d[c], top) / total * -mean;
+        for (int c = 0; c < PER; ++c) d[c] = top == -INFINITY ? 0.0f : d[c] * scale;
     }
+    constexpr int kN = kStep<T, PER>;
+    auto place_of = [](int e) { return e / kN % 16 * (PER + 1) + e / (16 * kN) * kN + e % kN; };
     // a token's choices are 16 lanes of one wave, and all different
-    __builtin_amdgcn_wave_barrier();
+    wave_order();
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        if (who[h] >= 0 && who[h] < 16 * PER) row[who[h] / PER * (PER + 1) + who[h] % PER] = w[h] * (renormalize ? g[h] - mean : g[h]);
-    __builtin_amdgcn_wave_barrier();
+        if (who[h] >= 0 && who[h] < 16 * PER) row[place_of(who[h])] = w[h] * (renormalize ? g[h] - mean : g[h]);
+    wave_order();
 #pragma unroll
     for (int c = 0; c < PER; ++c) d[c] += mine[c];
-    T *out = d_logits + t * experts + lane * PER;
-    if constexpr (VEC) {
-        constexpr int kStep = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER;
-        struct alignas(kStep * sizeof(T)) Piece {
-            T x[kStep];
-        };
+    T *const out = d_logits + t * experts;
 #pragma unroll
-        for (int c = 0; c < PER; c += kStep) {
-            Piece p;
+    for (int c = 0; c < PER; c += kN) {
+        const int e = expert_at<kN, PER, false>(lane, c);
+        if constexpr (VEC) {
+            Piece<T, kN> p;
 #pragma unroll
-            for (int i = 0; i < kStep; ++i) p.x[i] = from_f32<T>(d[c + i]);
-            *reinterpret_cast<Piece *>(out + c) = p;
+            for (int i = 0; i < kN; ++i) p.x[i] = from_f32<T>(d[c + i]);
+            *reinterpret_cast<Piece<T, kN> *>(out + e) = p;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (e + i < experts) out[e + i] = from_f32<T>(d[c + i]);
         }
-    } else {
-#pragma unroll
-        for (int c = 0; c < PER; ++c)
-            if (lane * PER + c < experts) out[c] = from_f32<T>(d[c]);
     }
 }
 
@@ -426,12 +508,14 @@ hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t to
     int bits = 1;
     while ((1 << bits) <= experts) ++bits;   // of the keys 0 .. experts
     const int rows_here = (int)(tokens < group ? tokens : group) * top_k;
-    const size_t lds = ((kChoose / 64 + (alone ? 1 : 0)) * (size_t)experts + rows_here) * 4;
     hipError_t e = by_type(type, [&](auto t) {
         using T = decltype(t);
         return by_experts(experts, [&](auto per) {
             constexpr int PER = decltype(per)::value;
+            constexpr int kChoose = choose_threads(PER);
             const bool vec = experts == 16 * PER && aligned(logits, 16) && stride * (int64_t)sizeof(T) % 16 == 0;
+            const int sums = (kChoose / 64 + (alone ? 1 : 0)) * experts, keys = kChoose / 16 * key_row(PER);
+            const size_t lds = (((rows_here + 3) & ~3) + (keys_in_lds(PER) && keys > sums ? keys : sums)) * sizeof(int);
             auto *kernel = alone ? (vec ? k_choose<T, PER, true, true> : k_choose<T, PER, false, true>)
                                  : (vec ? k_choose<T, PER, true, false> : k_choose<T, PER, false, false>);
             hipLaunchKernelGGL(kernel, many(groups), dim3(kChoose), lds, s, static_cast<const T *>(logits),
@@ -441,7 +525,7 @@ hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t to
         });
     });
     if (e != hipSuccess || alone) return e;
-    hipLaunchKernelGGL(k_scan_groups, dim3((unsigned)ceil_div(experts, 16)), dim3(kScanThreads), 0, s, hist,
+    hipLaunchKernelGGL(k_scan_groups, dim3((unsigned)ceil_div(experts, kScanExperts)), dim3(kScanThreads), 0, s, hist,
                        (int)groups, experts, count);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int64_t rows = tokens * top_k;
