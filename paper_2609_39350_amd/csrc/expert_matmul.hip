@@ -717,34 +717,30 @@ struct Fragments {
     }
 };
 
-// BQ x BP outputs a workgroup of WQ x WP waves.  STAGES tiles of 64 summands in LDS.
+// BQ x BP outputs from row q0 of the tile's rows by a workgroup of WQ x WP waves.  STAGES tiles of 64 summands in LDS.
 template <int KIND, typename T, typename O, bool GATHER, int BQ, int BP, int WQ, int WP, int STAGES>
-__global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
+__device__ inline void product_tile(const Args &args, const Tile &t, int64_t q0, u32x4 *lds)
 {
     constexpr bool kQAlong = KIND != kGradW, kPAlong = KIND == kForward;
     constexpr int kThreads = 64 * WQ * WP;
     constexpr int kTileQ = BQ * 8, kTile = (BQ + BP) * 8;   // of LDS, in 16 bytes
     constexpr int kFq = BQ / WQ / 16, kFp = BP / WP / 16;    // a wave's fragments
     constexpr int kQPlaces = BQ / 8, kPPlaces = BP / 8;
-    __shared__ u32x4 lds[STAGES * kTile];
     const ExpertProduct &a = args.a;
-    Tile t;
     Loader<kQAlong, BQ, kThreads, GATHER && KIND == kForward> lq;
     Loader<kPAlong, BP, kThreads, GATHER && KIND == kGradW> lp;
     int64_t q_end, p_end, out_row;
     int k_end;
     if constexpr (KIND == kGradW) {
-        if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, (uint32_t)workgroup(), t)) return;
         q_end = a.outputs;
         p_end = a.inputs;
         k_end = t.hi - t.lo;
         out_row = (int64_t)t.expert * a.outputs;
         if (k_end > 0) {
-            lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, t.lo, a.rows, (int64_t)t.q * BQ, q_end, k_end);
+            lq.begin(a.d_y, a.d_y_stride, nullptr, args.by_top_k, t.lo, a.rows, q0, q_end, k_end);
             lp.begin(a.x, a.x_stride, a.slot, args.by_top_k, t.lo, a.x_rows, (int64_t)t.p * BP, p_end, k_end);
         }
     } else {
-        if (!find_tile<BQ>(a.offset, a.experts, a.rows, args.p_tiles, workgroup(), t)) return;
         q_end = t.hi - t.lo;
         p_end = KIND == kForward ? a.outputs : a.inputs;
         k_end = t.expert == a.experts ? 0 : KIND == kForward ? (int)a.inputs : (int)a.outputs;
@@ -752,7 +748,7 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
         if (k_end > 0) {
             const char *w = static_cast<const char *>(a.w) + t.expert * a.outputs * a.inputs * 2;
             lq.begin(KIND == kForward ? a.x : a.d_y, KIND == kForward ? a.x_stride : a.d_y_stride, a.slot,
-                     args.by_top_k, t.lo, KIND == kForward ? a.x_rows : a.rows, (int64_t)t.q * BQ, q_end, k_end);
+                     args.by_top_k, t.lo, KIND == kForward ? a.x_rows : a.rows, q0, q_end, k_end);
             lp.begin(w, a.inputs, nullptr, args.by_top_k, 0, a.outputs, (int64_t)t.p * BP, p_end, k_end);
         }
     }
@@ -764,7 +760,7 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
     // rows over 64 or 256 uneven experts; not in the largest tile, whose whole tiles the tests cost 1 to 5 %.
     constexpr bool kSkip = KIND != kGradW && BQ < 256;
     const int some = !kSkip ? kFq : __builtin_amdgcn_readfirstlane(
-        (int)max((int64_t)0, min((int64_t)kFq, (q_end - (int64_t)t.q * BQ - wq + 15) / 16)));
+        (int)max((int64_t)0, min((int64_t)kFq, (q_end - q0 - wq + 15) / 16)));
     f32x4 acc[kFq][kFp] = {};
     const uint32_t lds0 = (uint32_t)(uintptr_t)(Shared *)lds;
     auto issue_one = [&](auto may_end, int j, int stage) {
@@ -875,8 +871,28 @@ __global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
             }
         }
     }
-    store_tile<O, BQ, BP, WQ, WP, STAGES * kTile>(lds, acc, static_cast<O *>(a.out) + out_row * p_end, (int64_t)t.q * BQ,
-                                                  q_end, (int64_t)t.p * BP, p_end);
+    store_tile<O, BQ, BP, WQ, WP, STAGES * kTile>(lds, acc, static_cast<O *>(a.out) + out_row * p_end, q0, q_end,
+                                                  (int64_t)t.p * BP, p_end);
+}
+
+template <int KIND, typename T, typename O, bool GATHER, int BQ, int BP, int WQ, int WP, int STAGES>
+__global__ __launch_bounds__(64 * WQ * WP) void k_product(const Args args)
+{
+    __shared__ u32x4 lds[STAGES * (BQ + BP) * 8];
+    const ExpertProduct &a = args.a;
+    Tile t;
+    if constexpr (KIND == kGradW) {
+        if (!find_grad_w_tile(a.offset, a.experts, a.rows, args.p_tiles, args.q_tiles, (uint32_t)workgroup(), t)) return;
+    } else {
+        if (!find_tile<BQ>(a.offset, a.experts, a.rows, args.p_tiles, workgroup(), t)) return;
+    }
+    const int64_t q0 = (int64_t)t.q * BQ;
+    // an expert's last tile of up to half the rows is a tile of half the rows
+    if constexpr (KIND != kGradW && BQ == 256) {
+        if (t.hi - t.lo - q0 <= BQ / 2)
+            return product_tile<KIND, T, O, GATHER, BQ / 2, BP, WQ, WP, STAGES>(args, t, q0, lds);
+    }
+    product_tile<KIND, T, O, GATHER, BQ, BP, WQ, WP, STAGES>(args, t, q0, lds);
 }
 
 // d_w: BQ x BP outputs of one expert a workgroup of four waves, 32 rows at a time, three tiles in LDS, two workgroups a
