@@ -1028,11 +1028,21 @@ hipError_t product(const ExpertProduct &a, hipStream_t s)
 {
     const int64_t some = a.rows / a.experts;   // rows an expert
     if constexpr (KIND == kGradW) {
+        // Up to 128 tiles of 256 x 256 leave CUs idle: tiles of a quarter, two workgroups a CU.  8 experts of 512 x 2,048 with
+        // 2,048 rows each: 45 us by 64 x 256, 47 by 128 x 256, 56 by 256 x 256, with uneven rows 78, 104, 126.  Many rows are
+        // for the largest: 16 of 4,096 x 7,168 with 512 rows: 1,051, 831, 759 us.
+        if (a.experts * a.outputs * a.inputs >> 16 <= 128) return launch_grad_w<T, O, 64, 256>(a, s);
         if (some < 512) return launch_grad_w<T, O, 128, 256>(a, s);
         return launch<KIND, T, O, 256, 256, 2, 4, 2>(a, s);
     } else {
-        if (some < 48) return launch<KIND, T, O, 64, 128, 2, 2, 3>(a, s);
-        if (some < 192) return launch<KIND, T, O, 128, 128, 2, 2, 2>(a, s);
+        // Tiles by the rows of an expert, which fill them or not, and smaller ones where there are too few for 256 CUs.
+        // us by 256 x 256, 128 x 128, 64 x 128: 8 experts of 512 x 2,048, rows 2,048: 39, 23, 18; 8,192: 40, 31, 38; 16,384:
+        // 42, 52, 58; 16 of 4,096 x 7,168, rows 32,768: 1,648, 2,092, 2,950.  d_x of 64 experts of 2,048 x 4,096 with 160
+        // rows each: 256 us by 256 x 256, 323 by 128 x 128, of 1,024 x 1,024 with uneven ones 53 and 43.
+        const int64_t large = a.rows * (KIND == kForward ? a.outputs : a.inputs) >> 16;   // tiles of 256 x 256
+        if (some < 48 || large <= 32) return launch<KIND, T, O, 64, 128, 2, 2, 3>(a, s);
+        if (some < (KIND == kGradX && large >= 256 ? 128 : 192) || large <= 80)
+            return launch<KIND, T, O, 128, 128, 2, 2, 2>(a, s);
         return launch<KIND, T, O, 256, 256, 2, 4, 2>(a, s);
     }
 }

@@ -787,3 +787,18 @@ def test_products_past_one_axis_of_workgroups():
     off = torch.tensor([0, cut, R], dtype=torch.int32, device="cuda")
     for y in (ops.expert_matmul(x, w, off), ops.expert_matmul_grad_x(x, w, off)):
         assert torch.equal(y[:cut], x[:cut] * 2) and torch.equal(y[cut:], x[cut:] * 0.5)
+
+
+# -------------------------------------------------- products large enough for the larger tiles
+@pytest.mark.parametrize("gather", [0, 2])
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("counts,N,K", [
+    # rows that end in the first and in the second half of a tile, one row, none; a last tile of summands that ends early
+    ([1000, 257, 384, 0, 129, 1, 1920, 128, 385], 1416, 1544),
+    ([4608, 64, 256, 320, 40], 1408, 1608),
+    # some 150 rows an expert
+    ([150 + (i * 37) % 41 - 20 for i in range(28)] + [0, 1, 17, 300], 1416, 1528),
+    ([150 + (i * 29) % 37 - 18 for i in range(32)], 520, 4104)])
+def test_products_larger_tiles(counts, N, K, dtype, gather):
+    say("larger tiles", len(counts), N, K, dtype, gather)
+    check_products(counts, 6 if gather == 0 else 0, N, K, dtype, gather)
