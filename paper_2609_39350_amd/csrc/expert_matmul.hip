@@ -565,13 +565,6 @@ __device__ inline void load_to_lds(const char *base, uint32_t offset, uint32_t t
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(scalar(base)), "s"(to)
                  : "memory");
 }
-// 4 bytes of each lane's line, for the cache's sake alone: they go to LDS that nobody reads
-__device__ inline void touch(const char *base, uint32_t offset, uint32_t to)
-{
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(scalar(base)), "s"(to)
-                 : "memory");
-}
-
 // One operand's tiles: kLoads pieces of 16 bytes for each of THREADS threads.
 // ALONG: SIDE rows of DEPTH summands.  Across: DEPTH summands of SIDE columns.
 // Rows and columns past the last are read as the last, their results go nowhere; summands past the last are read as
