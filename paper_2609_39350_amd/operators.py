@@ -16,6 +16,7 @@ is no fallback path: without the library the first call raises.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 
 import torch
 
@@ -94,9 +95,16 @@ def _on_device(name, t):
         raise ValueError(f"{name}: on {t.device}, which is not the current device")
 
 
-# The checks below run on every call: their messages are put together only where one is due.
+# The checks below run on every call, which a decoding step waits for: one expression where all is well, and only where it
+# is not the tests one by one, with their messages.
+_device = torch.cuda.current_device
+
+
 def _array(name, t, dtype, *shape):
     """A contiguous tensor of this type and shape (None in the shape: any)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous() \
+            and t.get_device() == _device():
+        return
     _on_device(name, t)
     if t.dtype != dtype:
         raise ValueError(f"{name}: {dtype}, not {t.dtype}")
@@ -186,7 +194,7 @@ def route_backward(logits, routing: Routing, d_weight, keep=None, renormalize=Tr
     _array("routing.expert", routing.expert, torch.int32, tokens, k)
     _array("routing.weight", routing.weight, torch.float32, tokens, k)
     _array("d_weight", d_weight, torch.float32, tokens, k)
-    d_logits = torch.empty((tokens, experts), dtype=logits.dtype, device=logits.device)
+    d_logits = logits.new_empty((tokens, experts))
     _check(_lib().hapmoe_route_backward(logits.data_ptr(), _TYPES[logits.dtype], stride, tokens, experts, k,
                                         _keep(keep, tokens), 1 if renormalize else 0, routing.expert.data_ptr(),
                                         routing.weight.data_ptr(), d_weight.data_ptr(), d_logits.data_ptr(),
@@ -196,12 +204,16 @@ def route_backward(logits, routing: Routing, d_weight, keep=None, renormalize=Tr
 
 # --------------------------------------------------- a token's expert outputs
 def _rows(name, t):
+    if isinstance(t, torch.Tensor) and t.dtype in _TYPES and t.dim() == 2 and t.shape[1] and t.is_contiguous() \
+            and t.get_device() == _device():
+        return
     if _matrix(name, t, _TYPES) != t.shape[1]:
         raise ValueError(f"{name}: contiguous")
 
 
 def _choices_of(place):
-    _array("place", place, torch.int32, None, None)
+    shape = getattr(place, "shape", ())
+    _array("place", place, torch.int32, *(shape if len(shape) == 2 else (None, None)))
     tokens, top_k = place.shape
     if not 1 <= top_k <= MAX_TOP_K:
         raise ValueError(f"place: 1 to {MAX_TOP_K} choices, not {top_k}")
@@ -215,8 +227,9 @@ def combine(y, place, weight=None):
     tokens, top_k = _choices_of(place)
     if weight is not None:
         _array("weight", weight, torch.float32, tokens, top_k)
-    out = torch.empty((tokens, y.shape[1]), dtype=y.dtype, device=y.device)
-    _check(_lib().hapmoe_combine(y.data_ptr(), _TYPES[y.dtype], y.shape[0], tokens, top_k, y.shape[1],
+    rows, hidden = y.shape
+    out = y.new_empty((tokens, hidden))
+    _check(_lib().hapmoe_combine(y.data_ptr(), _TYPES[y.dtype], rows, tokens, top_k, hidden,
                                  place.data_ptr(), None if weight is None else weight.data_ptr(), out.data_ptr(),
                                  _stream(y)), "hapmoe_combine")
     return out
@@ -268,7 +281,7 @@ def expert_matmul(x, w, offset, slot=None, top_k=1):
     _array("w", w, x.dtype, experts, None, x.shape[1])
     _need(w.shape[1] > 0, "w: no outputs")
     rows = _rows_of(x, slot)
-    y = torch.empty((rows, w.shape[1]), dtype=x.dtype, device=x.device)
+    y = x.new_empty((rows, w.shape[1]))
     _check(_lib().hapmoe_expert_matmul(x.data_ptr(), x.shape[0], stride, w.data_ptr(), _TYPES[x.dtype], rows, experts,
                                        w.shape[1], w.shape[2], offset.data_ptr(),
                                        None if slot is None else slot.data_ptr(), top_k, y.data_ptr(), _stream(x)),
@@ -283,7 +296,7 @@ def expert_matmul_grad_x(d_y, w, offset):
     experts = _experts_of(offset)
     _array("w", w, d_y.dtype, experts, d_y.shape[1], None)
     _need(w.shape[2] > 0, "w: no inputs")
-    d_x = torch.empty((d_y.shape[0], w.shape[2]), dtype=d_y.dtype, device=d_y.device)
+    d_x = d_y.new_empty((d_y.shape[0], w.shape[2]))
     _check(_lib().hapmoe_expert_matmul_grad_x(d_y.data_ptr(), stride, w.data_ptr(), _TYPES[d_y.dtype], d_y.shape[0],
                                               experts, w.shape[1], w.shape[2], offset.data_ptr(), d_x.data_ptr(),
                                               _stream(d_y)), "hapmoe_expert_matmul_grad_x")
@@ -311,7 +324,8 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
 
 
 # -------------------------------------------------------------- the optimizer
-_POINTER, _CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.is_contiguous
+_POINTER, _CONTIGUOUS, _NUMEL = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.numel
+_DEVICE, _DTYPE = torch.Tensor.get_device, operator.attrgetter("dtype")
 
 
 class AdamW:
@@ -378,8 +392,8 @@ class AdamW:
             if index != torch.cuda.current_device():
                 raise ValueError(f"the parameters' device {index} is not the current device")
             # list by list: a step over many small tensors waits for these checks
-            if ([g.dtype for g in grads].count(dtype) != n or [g.get_device() for g in grads].count(index) != n
-                    or [g.numel() for g in grads] != self._sizes or not all(map(_CONTIGUOUS, grads))):
+            if (set(map(_DTYPE, grads)) != {dtype} or set(map(_DEVICE, grads)) != {index}
+                    or list(map(_NUMEL, grads)) != self._sizes or not all(map(_CONTIGUOUS, grads))):
                 raise ValueError(f"grads: contiguous on device {index}, of one type and the parameters' sizes")
             a.grad_type = _TYPES[dtype]
         a.lr, a.beta1, a.beta2, a.eps, a.grad_scale, a.step = lr, beta1, beta2, eps, grad_scale, step
