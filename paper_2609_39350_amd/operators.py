@@ -102,8 +102,8 @@ _device = torch.cuda.current_device
 
 def _array(name, t, dtype, *shape):
     """A contiguous tensor of this type and shape (None in the shape: any)."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous() \
-            and t.get_device() == _device():
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == shape \
+            and t.is_contiguous() and t.get_device() == _device():
         return
     _on_device(name, t)
     if t.dtype != dtype:
@@ -204,8 +204,8 @@ def route_backward(logits, routing: Routing, d_weight, keep=None, renormalize=Tr
 
 # --------------------------------------------------- a token's expert outputs
 def _rows(name, t):
-    if isinstance(t, torch.Tensor) and t.dtype in _TYPES and t.dim() == 2 and t.shape[1] and t.is_contiguous() \
-            and t.get_device() == _device():
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _TYPES and t.dim() == 2 and t.shape[1] \
+            and t.is_contiguous() and t.get_device() == _device():
         return
     if _matrix(name, t, _TYPES) != t.shape[1]:
         raise ValueError(f"{name}: contiguous")
