@@ -15,6 +15,7 @@ is no fallback path: without the library the first call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import operator
 
@@ -73,8 +74,10 @@ def _check(code, what):
 
 
 try:   # the current stream's address without an object for it: 0.1 us of a call, where the object takes 2
-    from torch._C import _cuda_getCurrentRawStream as _stream_of
+    from torch._C import _cuda_getCurrentRawStream as _stream_of, _cuda_getDevice as _device
 except ImportError:
+    _device = torch.cuda.current_device
+
     def _stream_of(index):
         return torch.cuda.current_stream(index).cuda_stream
 
@@ -97,9 +100,6 @@ def _on_device(name, t):
 
 # The checks below run on every call, which a decoding step waits for: one expression where all is well, and only where it
 # is not the tests one by one, with their messages.
-_device = torch.cuda.current_device
-
-
 def _array(name, t, dtype, *shape):
     """A contiguous tensor of this type and shape (None in the shape: any)."""
     if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == shape \
@@ -371,6 +371,7 @@ class AdamW:
         self._table = (_Tensor * max(n, 1))()
         self._pointers = C.c_void_p * max(n, 1)
         self._args = _Args(copy_type=_TYPES[copies[0].dtype] if copies else 0, state_bits=self.state_bits)
+        self._args_at = C.byref(self._args)
         for i, t in enumerate(self._table[:n]):
             t.param, t.m, t.v, t.n = params[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr(), params[i].numel()
             t.copy = copies[i].data_ptr() if copies else None
@@ -389,7 +390,7 @@ class AdamW:
             dtype, index = grads[0].dtype, self._index
             if dtype not in _TYPES:
                 raise ValueError(f"grads: a floating type of 32 or 16 bits, not {dtype}")
-            if index != torch.cuda.current_device():
+            if index != _device():
                 raise ValueError(f"the parameters' device {index} is not the current device")
             # list by list: a step over many small tensors waits for these checks
             if (set(map(_DTYPE, grads)) != {dtype} or set(map(_DEVICE, grads)) != {index}
@@ -401,8 +402,9 @@ class AdamW:
         if skip is not None:
             _array("skip", skip, torch.int32, 1)
         a.d_skip = None if skip is None else skip.data_ptr()
-        _check(_lib().hapmoe_adamw(self._table, self._pointers(*map(_POINTER, grads)), n, C.byref(a),
-                                   _stream_of(torch.cuda.current_device())), "hapmoe_adamw")
+        pointers = array.array("Q", map(_POINTER, grads))   # held until the call returns
+        _check(_lib().hapmoe_adamw(self._table, pointers.buffer_info()[0], n, self._args_at,
+                                   _stream_of(torch.cuda.current_device() if n == 0 else index)), "hapmoe_adamw")
 
     def moments(self, dtype=torch.float32):
         """The values of m and v: two lists of tensors shaped like the parameters.  Moments in 8 bits are decoded
