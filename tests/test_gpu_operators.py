@@ -802,3 +802,31 @@ def test_products_past_one_axis_of_workgroups():
 def test_products_larger_tiles(counts, N, K, dtype, gather):
     say("larger tiles", len(counts), N, K, dtype, gather)
     check_products(counts, 6 if gather == 0 else 0, N, K, dtype, gather)
+
+
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("E,k", [(128, 8), (129, 5), (256, 8), (300, 32), (512, 17), (700, 8), (1024, 32)])
+def test_route_ties_and_closed_experts_of_wide_routers(E, k, renormalize):
+    """Many equal logits, of neighbouring lanes and within one; infinities, NaN, rows all closed or with fewer open experts
+    than choices."""
+    say("route ties", E, k, renormalize)
+    T = 70
+    logits = torch.randint(-2, 3, (T, E), generator=gen(E), device="cuda").float()
+    logits[torch.rand((T, E), generator=gen(1), device="cuda") < 0.1] = -math.inf
+    logits[torch.rand((T, E), generator=gen(2), device="cuda") < 0.05] = math.nan
+    logits[0], logits[1], logits[2], logits[3] = 0.0, -math.inf, math.nan, torch.finfo(torch.float32).min
+    logits[4] = -math.inf
+    logits[4, E - 1], logits[4, E // 2] = 1.0, 2.0
+    logits[5, 3], logits[5, E - 2] = math.inf, math.inf
+    logits[6] = torch.where(torch.arange(E, device="cuda") % 2 == 0, -0.0, 0.0)
+    logits[7] = -1.0
+    logits[7, E - 9:] = 1.0
+    for n in (9, T):   # one workgroup, several
+        x = logits[:n]
+        for dtype in (torch.float32, torch.bfloat16):
+            y = x.to(dtype)
+            r = ops.route(y, k, renormalize=renormalize)
+            ref = route_ref(y, k, None, renormalize)
+            check_routing(r, ref, E)
+            d = ops.route_backward(y, r, normal(3, n, k), renormalize=renormalize)
+            assert d.isfinite().all() and (d[y.isnan() | (y == -math.inf)] == 0).all()
