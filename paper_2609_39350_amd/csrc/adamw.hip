@@ -6,8 +6,10 @@
 // Every operation is a single fp32 one, rounded to nearest (no contraction), in
 // the order of the formula in the header.
 //
-// 537 M elements in 16 tensors, fp32 with a bf16 copy: 2,631 to 2,896 us by the card, 5.6 to 6.1 TB/s.  235 M, 8-bit moments, bf16 gradient and copy:
-// 730 to 850 us (16 bytes an element, 4.4 to 5.1 TB/s), their values 300 us.  24 tensors of 3,413: 4.7 us, a launch.
+// 537 M elements in 16 tensors, fp32 with a bf16 copy: 2,631 to 2,896 us by the
+// card, 5.6 to 6.1 TB/s.  235 M, 8-bit moments, bf16 gradient and copy: 730 to 850 us
+// (16 bytes an element, 4.4 to 5.1 TB/s), their values 300 us.  24 tensors of 3,413:
+// 4.7 us, a launch.
 #include "operators.h"
 
 namespace hapmoe {
