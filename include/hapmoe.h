@@ -526,7 +526,9 @@ int32_t hapmoe_combine(const void *d_y, int32_t type, int64_t rows, int64_t toke
 
 /* Gradients of hapmoe_combine, rows = tokens * top_k: d_d_y [rows][hidden],
  * row i = weight[slot[i]] d_out[slot[i] / top_k], 0 where slot[i] is -1, and
- * d_d_weight[t][j] = <d_out[t], y[place[t][j]]>, 0 where place is -1. */
+ * d_d_weight[t][j] = <d_out[t], y[place[t][j]]>, 0 where place is -1.  Both
+ * hold for any slot and place; where hapmoe_combine's gradient is wanted they
+ * have to be each other's inverse, as hapmoe_route writes them. */
 int32_t hapmoe_combine_backward(const void *d_d_out, const void *d_y, int32_t type, int64_t tokens, int32_t top_k,
                                 int64_t hidden, const int32_t *d_slot, const int32_t *d_place, const float *d_weight,
                                 void *d_d_y, float *d_d_weight, void *stream);

@@ -4,6 +4,8 @@
 // order and no atomics.  bf16, 8 choices, hidden 4,096: 4,096 tokens 60 us (5.1 TB/s),
 // backward 110 us (5.5 TB/s).  16 tokens of 7,168: 4.2 us, a launch and two dependent
 // loads.
+#include <type_traits>
+
 #include "operators.h"
 
 namespace hapmoe {
@@ -46,8 +48,11 @@ __global__ __launch_bounds__(kThreads) void k_combine(const T *__restrict__ y, i
 }
 
 // A wave a (token, choice): it reads d_out[t] (which the token's other choices read too, from the cache) and its row
-// of y once, and writes the row of d_y; the wave of row i also clears it where no choice has it.  ONCE: 1, y goes past the
-// caches, 2, d_y too.  us at 59, 268, 470 MB of y (bf16): 22.1, 118.6, 203 (0), 24.4, 102.2, 205 (1), 25.5, 111, 190 (2).
+// of y once, and writes the row of d_y where slot names this choice there, as place and slot of the router do.  Where they
+// do not agree each still has its own: d_weight[r] goes by place, and row r of d_y, by slot, has the wave of row r as its
+// writer, which also clears it where no choice has it.  Knowing whether they agree costs one more
+// dependent load: 106 us against 103 at 268 MB of y, nothing at 59 and 459.  ONCE: 1, y goes past the caches, 2, d_y too.  us
+// at 59, 268, 470 MB of y (bf16): 22.1, 118.6, 203 (0), 24.4, 102.2, 205 (1), 25.5, 111, 190 (2).
 template <typename T, bool VEC, int ONCE>
 __global__ __launch_bounds__(kThreads) void k_combine_backward(
     const T *__restrict__ d_out, const T *__restrict__ y, int64_t rows, int top_k, int64_t hidden,
@@ -56,17 +61,17 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(
 {
     constexpr int kStep = VEC ? 8 : 1;
     const int lane = threadIdx.x & 63;
-    const int64_t r = workgroup() * (kThreads / 64) + (threadIdx.x >> 6);
+    const int64_t r = workgroup() * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (r >= rows) return;
-    if ((uint32_t)slot[r] >= (uint64_t)rows) {
-        for (int64_t h = lane; h < hidden; h += 64) d_y[r * hidden + h] = from_f32<T>(0.0f);
-    }
-    const int p = place[r];
+    const int p = place[r], s = slot[r];
+    const float w = weight[r];
+    const bool has = (uint32_t)p < (uint64_t)rows, taken = (uint32_t)s < (uint64_t)rows;
+    const int back = slot[has ? p : 0], forth = place[taken ? s : 0];   // both on their way at once
+    const bool writes = has && back == r, left = !taken || forth != r;
     float dot = 0.0f;
-    if ((uint32_t)p < (uint64_t)rows) {
-        const T *g = d_out + r / top_k * hidden, *row = y + p * hidden;
+    auto pass = [&](auto write) {
+        const T *g = d_out + (int)r / top_k * hidden, *row = y + p * hidden;
         T *to = d_y + p * hidden;
-        const float w = weight[r];
 #pragma unroll 2
         for (int64_t h = lane * kStep; h < hidden; h += 64 * kStep) {
             if constexpr (VEC) {
@@ -78,18 +83,29 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(
                     dot += to_f32(a.v[i]) * to_f32(b.v[i]);
                     c.v[i] = from_f32<T>(w * to_f32(a.v[i]));
                 }
-                if constexpr (ONCE == 2)
+                if constexpr (!decltype(write)::value)
+                    continue;
+                else if constexpr (ONCE == 2)
                     store_once(to + h, c);
                 else
                     *reinterpret_cast<Vec8<T> *>(to + h) = c;
             } else {
                 dot += to_f32(g[h]) * to_f32(row[h]);
-                to[h] = from_f32<T>(w * to_f32(g[h]));
+                if constexpr (decltype(write)::value) to[h] = from_f32<T>(w * to_f32(g[h]));
             }
         }
-        dot = wave_reduce(dot, Sum());
-    }
+    };
+    if (writes)
+        pass(std::true_type());
+    else if (has)
+        pass(std::false_type());
+    dot = wave_reduce(dot, Sum());
     if (lane == 0) d_weight[r] = dot;
+    if (left) {
+        const T *g = taken ? d_out + s / top_k * hidden : nullptr;
+        const float other = taken ? weight[s] : 0.0f;
+        for (int64_t h = lane; h < hidden; h += 64) d_y[r * hidden + h] = from_f32<T>(taken ? other * to_f32(g[h]) : 0.0f);
+    }
 }
 
 template <typename T>
