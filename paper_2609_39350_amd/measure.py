@@ -148,17 +148,24 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
             "expert_tokens": got["routing"].count.cpu().numpy().astype(np.int64)}
 
 
-def apply(problem, device_type, measured):
+def apply(problem, device_type, measured, shared=None):
     """A problem whose device type has what was measured: the expert FFN's time (with its share over TP and CP as
     it was), the router's (with the rows' sum), and for all types the optimizer's time a parameter.  The router's
-    counts, if the whole layer ran, become those of the layer measured."""
+    counts, if the whole layer ran, become those of the layer measured.
+
+    What ran are a token's top_k routed experts.  shared: experts that every token takes beside them, each counted
+    as long as a routed one; None: what moe_ffn_mult has above top_k, which holds where it counts experts and not
+    an expert's size."""
     out = copy.deepcopy(problem)
     m, c, h = out["model"], out["cluster"], int(device_type)
     if not 0 <= h < int(c["n_types"]):
         raise ValueError(f"device type {h} of {c['n_types']}")
     c["eff"][h] = 1.0
     c["route_coef"][h] = (measured["route_ns"] + measured["combine_ns"]) / (measured["tokens"] * measured["hidden"])
-    one = measured["experts_ns"] / float(m["moe_ffn_mult"])   # Eq. 2 multiplies an expert's FFN time by this
+    k, mult = int(m["top_k"]), float(m["moe_ffn_mult"])
+    shared = max(0.0, mult - k) if shared is None else shared
+    # Eq. 2 multiplies t_ffn by moe_ffn_mult, for the routed and the shared experts together
+    one = measured["experts_ns"] * (k + shared) / k / (mult or k)
     moe = np.asarray(m["is_moe"]) == 1
     was = np.asarray(c["t_ffn"][h], dtype=np.float64)
     share = np.where(was[0, 0] > 0, was / np.maximum(was[0, 0], 1.0), 1.0)   # of a (TP, CP) of the whole
