@@ -3,12 +3,13 @@ router times, router statistics, optimizer time).
 
 One mixture-of-experts layer of a problem's model takes training steps on the operators of
 ``operators.py``: router, gated expert FFNs, the sum of each token's expert outputs, all of it
-backward, and AdamW over the experts.  ``apply`` puts what was measured in the place of one
-device type's entries, so that the planner weighs that type by what its operators take:
+backward, and AdamW over the experts.  Its weights and inputs are random.  ``apply`` puts what
+was measured in the place of one device type's entries, so that the planner weighs that type by
+what its operators take:
 
     python -m paper_2609_39350_amd.measure --config 2 --type 2
 
-prints the measurement and the plans before and after.
+prints the measurement and the plans before and after, both with the workload's router counts.
 """
 from __future__ import annotations
 
@@ -148,10 +149,13 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
             "expert_tokens": got["routing"].count.cpu().numpy().astype(np.int64)}
 
 
-def apply(problem, device_type, measured, shared=None):
+def apply(problem, device_type, measured, shared=None, counts=True):
     """A problem whose device type has what was measured: the expert FFN's time (with its share over TP and CP as
-    it was), the router's (with the rows' sum), and for all types the optimizer's time a parameter.  The router's
-    counts, if the whole layer ran, become those of the layer measured.
+    it was), the router's (with the rows' sum), and for all types the optimizer's time a parameter.
+
+    counts: the router's counts, if the whole layer ran, become those of the layer measured.  They are those of a
+    random router, whose experts are taken as unevenly as ``Layer``'s skew says: False where the problem's come of a
+    model's own router.
 
     What ran are a token's top_k routed experts.  shared: experts that every token takes beside them, each counted
     as long as a routed one; None: what moe_ffn_mult has above top_k, which holds where it counts experts and not
@@ -173,7 +177,7 @@ def apply(problem, device_type, measured, shared=None):
     c["t_dense"][h] = c["t_dense"][h] - c["t_ffn"][h] + ffn
     c["t_ffn"][h] = ffn
     out["params"]["opt_coef"] = measured["opt_ns_per_param"]
-    if measured["part"] == 1:
+    if counts and measured["part"] == 1:
         m["expert_tokens"][measured["layer"]] = measured["expert_tokens"]
     return out
 
@@ -193,7 +197,7 @@ def main(argv=None):
     print(f"experts {got['experts_ns'] / 1e3:.0f} us ({flops / got['experts_ns'] / 1e3:.0f} TFLOP/s), router "
           f"{got['route_ns'] / 1e3:.0f} us, rows' sum {got['combine_ns'] / 1e3:.0f} us, optimizer "
           f"{got['opt_ns_per_param'] * 1e3:.2f} ps a parameter")
-    for name, q in (("as given", problem), ("measured", apply(problem, a.type, got))):
+    for name, q in (("as given", problem), ("measured", apply(problem, a.type, got, counts=False))):
         plan = binding.Planner(q, "cuda:0").run()
         print(f"{name}: (PP, TP, CP, DP, EP, TPE) {plan['config']}, B {plan['n_micro']}, {plan['objective']} ns, layers "
               f"{plan['layers']}")

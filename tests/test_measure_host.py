@@ -63,3 +63,37 @@ def test_a_factor_of_zero():
     q = measure.apply(problem, 0, made_up(problem))
     binding.validate(q)
     assert np.all(expert_term(q, 0) == 0)
+
+
+def test_counts_of_a_profile_stay():
+    """The measured layer's router is random: its counts replace those of a problem only where they are asked for."""
+    problem = workloads.config(2)
+    got = made_up(problem)
+    tokens = problem["model"]["expert_tokens"].copy()
+    kept = measure.apply(problem, 1, got, counts=False)
+    assert np.array_equal(kept["model"]["expert_tokens"], tokens)
+    taken = measure.apply(problem, 1, got, counts=True)
+    assert np.array_equal(taken["model"]["expert_tokens"][got["layer"]], got["expert_tokens"])
+    for q in (kept, taken):
+        assert np.array_equal(problem["model"]["expert_tokens"], tokens)
+        assert np.array_equal(np.delete(q["model"]["expert_tokens"], got["layer"], 0), np.delete(tokens, got["layer"], 0))
+
+
+def test_command_plans_with_the_workloads_counts(monkeypatch, capsys):
+    planned = []
+
+    class Planner:
+        def __init__(self, problem, device):
+            planned.append(problem)
+
+        def run(self):
+            return {"config": (1,) * 6, "n_micro": 1, "objective": 1, "layers": [1]}
+
+    problem = workloads.config(3)
+    monkeypatch.setattr(measure, "measure", lambda p, **kw: made_up(p))
+    monkeypatch.setattr(measure.binding, "Planner", Planner)
+    measure.main(["--config", "3", "--type", "1"])
+    assert len(planned) == 2 and len(capsys.readouterr().out.splitlines()) == 4
+    for q in planned:
+        assert np.array_equal(q["model"]["expert_tokens"], problem["model"]["expert_tokens"])
+    assert not np.array_equal(planned[0]["cluster"]["t_ffn"][1], planned[1]["cluster"]["t_ffn"][1])
