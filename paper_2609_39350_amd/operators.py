@@ -28,6 +28,7 @@ MAX_EXPERTS = 1024
 MAX_TOP_K = 32
 BLOCK = 256   # elements that share an exponent in an 8-bit moment
 
+_POINTER = torch.Tensor.data_ptr
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _LIB = None
 
@@ -94,7 +95,7 @@ def _need(ok, what):
 def _on_device(name, t):
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
         raise ValueError(f"{name}: a tensor on the GPU")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != _device():
         raise ValueError(f"{name}: on {t.device}, which is not the current device")
 
 
@@ -139,7 +140,7 @@ class Routing:
 
     expert [tokens, top_k] int32 (-1: none), weight [tokens, top_k] fp32, count [experts] int32,
     offset [experts + 1] int32, slot [tokens * top_k] int32 and place [tokens, top_k] int32 as in
-    include/hapmoe.h.
+    include/hapmoe.h.  A Routing whose tensors were replaced is refused.
     """
 
     def __init__(self, tokens: int, experts: int, top_k: int, device="cuda"):
@@ -156,8 +157,11 @@ class Routing:
         self.slot = torch.empty(tokens * top_k, **i32)
         self.place = torch.empty((tokens, top_k), **i32)
         self._ws = torch.empty(need.value, dtype=torch.uint8, device=device)
-        self._outputs = tuple(t.data_ptr() for t in (self.weight, self.expert, self.count, self.offset, self.slot,
-                                                     self.place, self._ws)) + (need.value,)
+        self._outputs = self._addresses()
+        self._ws_bytes = need.value
+
+    def _addresses(self):
+        return tuple(map(_POINTER, (self.weight, self.expert, self.count, self.offset, self.slot, self.place, self._ws)))
 
 
 def _keep(keep, tokens):
@@ -178,8 +182,10 @@ def route(logits, top_k: int, keep=None, renormalize=True, out: Routing = None) 
     else:
         _need((out.tokens, out.experts, out.top_k) == (tokens, experts, top_k) and
               out.expert.device == logits.device, "out: made for other sizes or another device")
+        # the call writes to these addresses, whatever the attributes name by now
+        _need(out._addresses() == out._outputs, "out: a buffer was replaced")
     _check(_lib().hapmoe_route(logits.data_ptr(), _TYPES[logits.dtype], stride, tokens, experts, top_k,
-                               _keep(keep, tokens), 1 if renormalize else 0, *out._outputs, _stream(logits)),
+                               _keep(keep, tokens), 1 if renormalize else 0, *out._outputs, out._ws_bytes, _stream(logits)),
            "hapmoe_route")
     return out
 
@@ -324,7 +330,7 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
 
 
 # -------------------------------------------------------------- the optimizer
-_POINTER, _CONTIGUOUS, _NUMEL = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.numel
+_CONTIGUOUS, _NUMEL = torch.Tensor.is_contiguous, torch.Tensor.numel
 _DEVICE, _DTYPE = torch.Tensor.get_device, operator.attrgetter("dtype")
 
 
