@@ -341,7 +341,8 @@ class AdamW:
     (int8, one for every 256 elements, the last of a tensor fewer); copies: None, or a bf16 or fp16
     tensor for each parameter that gets its new value; weight_decay: one number, or one for each.
     All contiguous, and kept alive by this object, which holds nothing else: state that starts at
-    zero is zeros of these tensors.
+    zero is zeros of these tensors.  Their memory is that of the moment this object is made: after
+    one was given other storage (``p.data = q``, ``set_``, a resize) make another AdamW of them.
     """
 
     def __init__(self, params, m, v, copies=None, m_exp=None, v_exp=None, weight_decay=0.0):
@@ -372,7 +373,9 @@ class AdamW:
                 _array(f"copies[{i}]", copies[i], copies[0].dtype, *shape)
             _need(decay[i] >= 0, f"weight_decay[{i}]: at least 0")
         self._index = params[0].get_device() if n else None
-        self._kept = (params, m, v, copies, m_exp, v_exp)
+        self._kept = (params, m, v)
+        # what the table's addresses lie in: a tensor given other storage would let go of it
+        self._memory = [t.detach() for x in (params, m, v, copies, m_exp, v_exp) if x is not None for t in x]
         self._sizes = [p.numel() for p in params]
         self._table = (_Tensor * max(n, 1))()
         self._pointers = C.c_void_p * max(n, 1)
@@ -415,7 +418,7 @@ class AdamW:
     def moments(self, dtype=torch.float32):
         """The values of m and v: two lists of tensors shaped like the parameters.  Moments in 8 bits are decoded
         to fp32 or bf16 (``hapmoe_adamw_moments``); fp32 ones are the state's own tensors."""
-        params, m, v = self._kept[:3]
+        params, m, v = self._kept
         if self.state_bits == 32:
             _need(dtype == torch.float32, "moments in 32 bits are torch.float32")
             return list(m), list(v)

@@ -31,3 +31,29 @@ def test_a_routing_with_a_replaced_buffer_is_refused(name, how):
     assert (getattr(r, name) == 5).all()
     again = ops.route(logits, 2, out=ops.Routing(80, 16, 2))
     assert all(torch.equal(getattr(again, n), w) for n, w in want.items())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_an_optimizer_keeps_the_memory_that_it_was_made_on(bits):
+    """A parameter, copy or moment given other storage afterwards: the step still works on what it was made on, which
+    nothing else gets in the meantime; an optimizer made anew works on the new."""
+    n = 4 << 20   # blocks of their own, which the allocator would give to the next tensor of the size
+    p, c = normal(1, n), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = [normal(2, n)]
+    if bits == 32:
+        m, v, small = normal(3, n), normal(4, n).square(), {}
+    else:
+        m, v = (torch.full((n,), 40, dtype=torch.uint8, device="cuda") for _ in range(2))
+        small = {k: [torch.full((n // 256,), -10, dtype=torch.int8, device="cuda")] for k in ("m_exp", "v_exp")}
+    state = [p, c, m, v] + [x[0] for x in small.values()]
+    before = [t.clone() for t in state]
+    opt = ops.AdamW([p], [m], [v], copies=[c], **small)
+    for t in state:
+        t.data = t.data.clone()
+    others = [torch.zeros_like(t) for t in state for _ in range(2)]   # takes freed memory, if there is any
+    opt.step(g, lr=1e-2, step=5, seed=1)
+    assert all((t == 0).all() for t in others)
+    assert all(torch.equal(a, b) for a, b in zip(state, before))
+    opt = ops.AdamW([p], [m], [v], copies=[c], **small)
+    opt.step(g, lr=1e-2, step=5, seed=1)
+    assert not torch.equal(p, before[0]) and torch.equal(c, p.bfloat16())
