@@ -594,7 +594,11 @@ typedef struct hapmoe_adamw_args {
  * 2^-111 on).  Both round up with the probability of what is cut off, so that
  * the running means do not drift or stick; a v above 0 stays above 0.  The 16
  * random bits of each are a fixed function of seed and of the element's index
- * over all tensors, each counted in whole blocks of 256. */
+ * over all tensors, each counted in whole blocks of 256.  All of args but what
+ * d_skip points to is read before the call returns: a captured call replays
+ * with the same lr, step and seed, so with state_bits = 8 every replay rounds an
+ * element by the same bits, and means drift or stick.  Train 8-bit moments by a
+ * call a step. */
 int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, const void *const *grads, int32_t n_tensors,
                      const hapmoe_adamw_args *args, void *stream);
 

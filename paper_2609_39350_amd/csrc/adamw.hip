@@ -1,7 +1,8 @@
 // AdamW over many tensors, moments in fp32 or in 8 bits.  Bound by HBM: every
 // operand is read once and written once.  The tensors' addresses travel in the
 // kernel's arguments (up to kTensors a launch), so a step copies nothing to the
-// device and may be captured.
+// device and may be captured.  So do the numbers of the step: a captured one
+// replays with the lr, step and seed of its capture.
 //
 // Every operation is a single fp32 one, rounded to nearest (no contraction), in
 // the order of the formula in the header.

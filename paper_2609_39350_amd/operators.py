@@ -390,7 +390,8 @@ class AdamW:
     def step(self, grads, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, seed=0, skip=None):
         """One step from one gradient for each parameter (contiguous, all of one type).  step: 1 for the first.
         grad_scale multiplies the gradients.  seed: of the 8-bit moments' roundings, another for every step.
-        skip: an int32 tensor of one element on the device; if it is not 0 nothing changes."""
+        skip: an int32 tensor of one element on the device; if it is not 0 nothing changes.
+        A captured step replays with the numbers of its capture: only with moments in 32 bits, at one lr and step."""
         n = len(self._sizes)
         if len(grads) != n:
             raise ValueError(f"grads: {n}, not {len(grads)}")

@@ -57,3 +57,33 @@ def test_an_optimizer_keeps_the_memory_that_it_was_made_on(bits):
     opt = ops.AdamW([p], [m], [v], copies=[c], **small)
     opt.step(g, lr=1e-2, step=5, seed=1)
     assert not torch.equal(p, before[0]) and torch.equal(c, p.bfloat16())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_captured_step_replays_with_the_numbers_of_its_capture(bits):
+    """lr, step and seed are read by the call: every replay is the call with the same ones."""
+    def make():
+        p, small = normal(1, 3000), {}
+        if bits == 8:
+            small = {k: [torch.zeros(12, dtype=torch.int8, device="cuda")] for k in ("m_exp", "v_exp")}
+        m, v = (torch.zeros(3000, dtype=torch.uint8 if bits == 8 else torch.float32, device="cuda") for _ in range(2))
+        return [p, m, v], ops.AdamW([p], [m], [v], **small)
+
+    g = [normal(2, 3000)]
+    numbers = {"lr": 1e-2, "step": 3, "seed": 9}
+    (captured, a), (eager, b) = make(), make()
+    start = [t.clone() for t in captured]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        make()[1].step(g, **numbers)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step(g, **numbers)
+    assert all(torch.equal(x, y) for x, y in zip(captured, start))
+    for _ in range(3):
+        graph.replay()
+        b.step(g, **numbers)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(captured, eager))
