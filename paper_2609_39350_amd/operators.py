@@ -10,8 +10,9 @@ parameter -- are quantities of these operators:
 
 Thin calls of the C functions in include/hapmoe.h, which states each formula.  Tensors are on
 the current device; work is enqueued on its current stream and outputs are allocated there
-unless they are given.  A wrong argument raises ValueError before anything is launched.  There
-is no fallback path: without the library the first call raises.
+unless they are given.  A tensor, size or number that an operator cannot take raises ValueError
+before anything is launched.  There is no fallback path: without the library the first call
+raises.
 """
 from __future__ import annotations
 
@@ -24,6 +25,7 @@ import torch
 from . import binding
 
 F32, BF16, F16 = 0, 1, 2
+INVAL = -1
 MAX_EXPERTS = 1024
 MAX_TOP_K = 32
 BLOCK = 256   # elements that share an exponent in an 8-bit moment
@@ -69,9 +71,13 @@ def _lib():
     return _LIB
 
 
+class InvalidArgument(binding.HapmoeError, ValueError):
+    """A size or number that the C call refuses."""
+
+
 def _check(code, what):
     if code != 0:
-        raise binding.HapmoeError(code, what)
+        raise (InvalidArgument if code == INVAL else binding.HapmoeError)(code, what)
 
 
 try:   # the current stream's address without an object for it: 0.1 us of a call, where the object takes 2
@@ -167,6 +173,7 @@ class Routing:
 def _keep(keep, tokens):
     if keep is None:
         return None
+    _on_device("keep", keep)
     _array("keep", keep, torch.uint8 if keep.dtype == torch.uint8 else torch.bool, tokens)
     return keep.data_ptr()
 
@@ -263,10 +270,12 @@ def combine_backward(d_out, y, slot, place, weight):
 _HALF = (torch.bfloat16, torch.float16)
 
 
-def _rows_of(x, slot):
+def _rows_of(x, slot, top_k):
     if slot is None:
         return x.shape[0]
     _array("slot", slot, torch.int32, None)
+    if not -2**31 <= top_k < 2**31:   # the call's 32 bits; it refuses those below 1
+        raise ValueError(f"top_k: at least 1 and below 2^31, not {top_k}")
     return slot.shape[0]
 
 
@@ -286,7 +295,7 @@ def expert_matmul(x, w, offset, slot=None, top_k=1):
     experts = _experts_of(offset)
     _array("w", w, x.dtype, experts, None, x.shape[1])
     _need(w.shape[1] > 0, "w: no outputs")
-    rows = _rows_of(x, slot)
+    rows = _rows_of(x, slot, top_k)
     y = x.new_empty((rows, w.shape[1]))
     _check(_lib().hapmoe_expert_matmul(x.data_ptr(), x.shape[0], stride, w.data_ptr(), _TYPES[x.dtype], rows, experts,
                                        w.shape[1], w.shape[2], offset.data_ptr(),
@@ -315,7 +324,7 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
     step = _matrix("d_y", d_y, _HALF)
     stride = _matrix("x", x, (d_y.dtype,))
     experts = _experts_of(offset)
-    rows = _rows_of(x, slot)
+    rows = _rows_of(x, slot, top_k)
     if dtype not in (torch.float32, d_y.dtype):
         raise ValueError(f"dtype: torch.float32 or {d_y.dtype}, not {dtype}")
     if rows != d_y.shape[0]:
@@ -359,15 +368,18 @@ class AdamW:
         self.copy_type = None
         state = torch.float32 if self.state_bits == 32 else torch.uint8
         for i, p in enumerate(params):
+            _on_device(f"params[{i}]", p)
             shape = tuple(p.shape)
             _array(f"params[{i}]", p, torch.float32, *shape)
             for name, x in (("m", m), ("v", v)):
+                _on_device(f"{name}[{i}]", x[i])
                 _need(x[i].numel() == p.numel(), f"{name}[{i}]: {p.numel()} elements, not {x[i].numel()}")
                 _array(f"{name}[{i}]", x[i], state, *x[i].shape)
             for name, x in (("m_exp", m_exp), ("v_exp", v_exp)):
                 if x is not None:
                     _array(f"{name}[{i}]", x[i], torch.int8, -(-p.numel() // BLOCK))
             if copies is not None:
+                _on_device(f"copies[{i}]", copies[i])
                 _need(copies[i].dtype in _HALF and copies[i].dtype == copies[0].dtype,
                       f"copies[{i}]: all torch.bfloat16 or all torch.float16")
                 _array(f"copies[{i}]", copies[i], copies[0].dtype, *shape)
@@ -397,16 +409,22 @@ class AdamW:
             raise ValueError(f"grads: {n}, not {len(grads)}")
         a = self._args
         if n:
-            dtype, index = grads[0].dtype, self._index
-            if dtype not in _TYPES:
-                raise ValueError(f"grads: a floating type of 32 or 16 bits, not {dtype}")
+            index = self._index
             if index != _device():
                 raise ValueError(f"the parameters' device {index} is not the current device")
             # list by list: a step over many small tensors waits for these checks
-            if (set(map(_DTYPE, grads)) != {dtype} or set(map(_DEVICE, grads)) != {index}
-                    or list(map(_NUMEL, grads)) != self._sizes or not all(map(_CONTIGUOUS, grads))):
-                raise ValueError(f"grads: contiguous on device {index}, of one type and the parameters' sizes")
+            try:
+                dtype = grads[0].dtype
+                fine = (set(map(_DTYPE, grads)) == {dtype} and dtype in _TYPES and set(map(_DEVICE, grads)) == {index}
+                        and list(map(_NUMEL, grads)) == self._sizes and all(map(_CONTIGUOUS, grads)))
+            except (AttributeError, TypeError):   # not all of them are tensors
+                fine = False
+            if not fine:
+                raise ValueError(f"grads: contiguous tensors on device {index}, of one floating type of 32 or 16 bits and "
+                                 "the parameters' sizes")
             a.grad_type = _TYPES[dtype]
+        if not -2**63 <= step < 2**63:   # the call's 64 bits; it refuses those below 1
+            raise ValueError(f"step: {step}")
         a.lr, a.beta1, a.beta2, a.eps, a.grad_scale, a.step = lr, beta1, beta2, eps, grad_scale, step
         a.seed = seed & (2**64 - 1)
         if skip is not None:
