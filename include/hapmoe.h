@@ -534,8 +534,10 @@ int32_t hapmoe_combine_backward(const void *d_d_out, const void *d_y, int32_t ty
                                 void *d_d_y, float *d_d_weight, void *stream);
 
 /* Products grouped by expert.  Expert e has rows offset[e] .. offset[e + 1] of
- * `rows` rows (offset[0] = 0; any number each, none included) and the matrix
- * w[e] [outputs][inputs].  type BF16 or F16, products summed in fp32. */
+ * `rows` rows (offset[0] = 0 and none below the one before; any number each,
+ * none included) and the matrix w[e] [outputs][inputs].  type BF16 or F16,
+ * products summed in fp32.  Other offsets leave rows that no expert or two have
+ * without a defined value; nothing outside the arrays is touched. */
 
 /* y[i] = w[e(i)] x[i]  ([rows][outputs]); with d_slot, x[slot[i] / top_k] in
  * place of x[i], x having x_rows rows `x_stride` elements apart (slot -1: a row

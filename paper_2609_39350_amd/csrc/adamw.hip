@@ -220,10 +220,9 @@ __device__ inline void update(const Batch &b, const Entry &t, int64_t i, int n)
             em = k < n ? Max()(em, exponent_field(m[k])) : em;
             ev = k < n ? Max()(ev, exponent_field(v[k])) : ev;
         }
-        // the largest exponents of the block, both in one reduction
-        const int both = wave_reduce(em << 16, Max()), other = wave_reduce(ev, Max());
-        em = Max()(Min()(both >> 16, 254) - 127, -119) - 7;
-        ev = Max()(Min()(other, 254) - 127, -111) - 15;
+        // the largest exponents of the block
+        em = Max()(Min()(wave_reduce(em, Max()), 254) - 127, -119) - 7;
+        ev = Max()(Min()(wave_reduce(ev, Max()), 254) - 127, -111) - 15;
         if (n <= 0) return;
         const float sm = power_of_two(-em), sv = power_of_two(-ev);
         uint32_t cm = 0, cv = 0;

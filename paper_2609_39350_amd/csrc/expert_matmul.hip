@@ -561,8 +561,8 @@ __device__ inline const char *scalar(const char *p)
 }
 
 // 16 bytes a lane from memory to LDS at `to` (the wave's first lane; the others follow), counted by vmcnt alone: the
-// caller waits for it, and the compiler, which would wait for it at the next LDS read, does not see it.  Nothing else
-// here uses m0.
+// caller waits for it, and the compiler, which would wait for it at the next LDS read, does not see it.  m0 is a
+// register that the compiler keeps nothing in between instructions, and nothing else here uses it.
 __device__ inline void load_to_lds(uint64_t from, uint32_t to)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");

@@ -21,7 +21,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // the last z that exceed n are the kernel's to leave out.
 inline dim3 many(int64_t n, unsigned y = 1)
 {
-    constexpr int64_t kMost = int64_t(1) << 22;   // of up to 1,024 threads
+    constexpr int64_t kMost = int64_t(1) << 22;   // of up to 512 threads
     return n <= kMost ? dim3((unsigned)n, y) : dim3((unsigned)kMost, y, (unsigned)ceil_div(n, kMost));
 }
 __device__ inline int64_t workgroup() { return (int64_t)blockIdx.z * gridDim.x + blockIdx.x; }
