@@ -510,6 +510,10 @@ hipError_t by_size(const ExpertProduct &a, hipStream_t s)
 {
     if (a.inputs < 8 || a.outputs < 8) return launch<KIND, T, O, GATHER, true, 64, 1>(a, s);
     const int64_t p_size = KIND == kForward ? a.outputs : a.inputs;
+    // us by 64 x 64, by 128 x 128.  Few tiles, or few rows an expert, favour the smaller: 8 experts of 1,093 x 1,093, y: 1,024
+    // rows (72 tiles) 18, 24; 64 experts, 4,096 rows (288 tiles) 39, 54.  At 512 tiles of 512 rows an expert the larger are
+    // ahead (8 of 2,047 x 2,049: y 86, 55; d_x 100, 90; d_w of 552 tiles 25, 25), with 1,024 rows an expert by more: 175, 103;
+    // 188, 136; 209, 147.
     const int64_t tiles = ceil_div(KIND == kGradW ? a.experts * a.outputs : a.rows, 128) * ceil_div(p_size, 128);
     if (tiles < 1024) return launch<KIND, T, O, GATHER, false, 64, 4>(a, s);
     return launch<KIND, T, O, GATHER, false, 128, 2>(a, s);
@@ -1038,7 +1042,9 @@ hipError_t product(const ExpertProduct &a, hipStream_t s)
         // Tiles by the rows of an expert, which fill them or not, and smaller ones where there are too few for 256 CUs.
         // us by 256 x 256, 128 x 128, 64 x 128: 8 experts of 512 x 2,048, rows 2,048: 39, 23, 18; 8,192: 40, 31, 38; 16,384:
         // 42, 52, 58; 16 of 4,096 x 7,168, rows 32,768: 1,648, 2,092, 2,950.  d_x of 64 experts of 2,048 x 4,096 with 160
-        // rows each: 256 us by 256 x 256, 323 by 128 x 128, of 1,024 x 1,024 with uneven ones 53 and 43.
+        // rows each: 256 us by 256 x 256, 323 by 128 x 128, of 1,024 x 1,024 with uneven ones 53 and 43.  64 x 128 against
+        // 128 x 128, 64 experts of 2,048 x 4,096, uneven rows, on average 32: y 195, 221, d_x 214, 216; 48: 210, 232, 229, 221;
+        // 96: 255, 237, 270, 260.
         const int64_t large = a.rows * (KIND == kForward ? a.outputs : a.inputs) >> 16;   // tiles of 256 x 256
         if (some < 48 || large <= 32) return launch<KIND, T, O, 64, 128, 2, 2, 3>(a, s);
         if (some < (KIND == kGradX && large >= 256 ? 128 : 192) || large <= 80)
@@ -1053,8 +1059,9 @@ hipError_t product(const ExpertProduct &a, hipStream_t s)
 bool whole_vectors(const ExpertProduct &a)
 {
     constexpr int64_t kFar = int64_t(1) << 22;   // 256 rows this many elements long are within 32-bit offsets
-    return a.inputs <= kFar && a.outputs <= kFar && a.x_stride <= kFar && a.d_y_stride <= kFar && a.outputs % 8 == 0 && a.inputs % 8 == 0 && a.x_stride % 8 == 0 && a.d_y_stride % 8 == 0 &&
-           aligned(a.x, 16) && aligned(a.w, 16) && aligned(a.d_y, 16) && aligned(a.out, 16);
+    return a.inputs <= kFar && a.outputs <= kFar && a.x_stride <= kFar && a.d_y_stride <= kFar && a.outputs % 8 == 0 &&
+           a.inputs % 8 == 0 && a.x_stride % 8 == 0 && a.d_y_stride % 8 == 0 && aligned(a.x, 16) && aligned(a.w, 16) &&
+           aligned(a.d_y, 16) && aligned(a.out, 16);
 }
 
 template <int KIND, typename T, typename O>

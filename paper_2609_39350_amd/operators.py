@@ -11,8 +11,8 @@ parameter -- are quantities of these operators:
 Thin calls of the C functions in include/hapmoe.h, which states each formula.  Tensors are on
 the current device; work is enqueued on its current stream and outputs are allocated there
 unless they are given.  A tensor, size or number that an operator cannot take raises ValueError
-before anything is launched.  There is no fallback path: without the library the first call
-raises.
+before anything is launched.  No call records a graph for automatic differentiation: gradients
+are calls of their own.  There is no fallback path: without the library the first call raises.
 """
 from __future__ import annotations
 
