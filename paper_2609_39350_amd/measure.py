@@ -25,13 +25,23 @@ from . import binding, operators, workloads
 STATE_BYTES = {32: 18, 8: 12}   # of an expert parameter on the GPU: copy, gradient, master and moments
 
 
+def router_forward(x, router, top_k):
+    logits = x @ router.T
+    return logits, operators.route(logits, top_k)
+
+
+def router_backward(x, router, logits, routing, d_weight):
+    """The gradients of the router's matrix and, through it, of x in fp32."""
+    d_logits = operators.route_backward(logits, routing, d_weight)
+    return d_logits.T @ x, (d_logits @ router).float()
+
+
 def layer_step(x, router, experts, d_out, top_k, mark=lambda name: None):
     """One layer forward and backward.  x [tokens, hidden], router [n_experts, hidden], experts: the gate, up
     and down matrices [n_experts, width, hidden], the same, [n_experts, hidden, width], d_out: the gradient of the
     output.  Returns the routing, the output and the gradients; calls mark(name) where a part of the layer ends."""
     gate, up, down = experts
-    logits = x @ router.T
-    r = operators.route(logits, top_k)
+    logits, r = router_forward(x, router, top_k)
     mark("route")
     g = operators.expert_matmul(x, gate, r.offset, slot=r.slot, top_k=top_k)
     u = operators.expert_matmul(x, up, r.offset, slot=r.slot, top_k=top_k)
@@ -53,9 +63,8 @@ def layer_step(x, router, experts, d_out, top_k, mark=lambda name: None):
     mark("experts")
     d_x = operators.combine(d_rows[0], r.place).float() + operators.combine(d_rows[1], r.place).float()
     mark("combine")
-    d_logits = operators.route_backward(logits, r, d_weight)
-    d_router = d_logits.T @ x
-    d_x += (d_logits @ router).float()
+    d_router, d_rest = router_backward(x, router, logits, r, d_weight)
+    d_x += d_rest
     mark("route")
     return {"routing": r, "out": out, "d_x": d_x.to(x.dtype), "d_router": d_router,
             "d_experts": (d_gate, d_up, d_down)}
@@ -102,12 +111,50 @@ class Layer:
         return got
 
 
+def _router_step(tokens, hidden, experts, top_k, seed):
+    """The router of a layer of this size, forward and backward, by itself."""
+    layer = Layer(tokens, hidden, 1, experts, top_k, seed=seed)
+    d_weight = torch.ones((tokens, top_k), device="cuda")
+    d_x = torch.zeros((tokens, hidden), device="cuda")
+
+    def step(mark):
+        logits, r = router_forward(layer.x, layer.router, top_k)
+        _, d_rest = router_backward(layer.x, layer.router, logits, r, d_weight)
+        d_x.add_(d_rest)
+        mark("route")
+    return step
+
+
+def _times(step, warmup, steps):
+    """What the last of warmup + steps calls of step(mark) returned, and the median ns of what it marks, without the
+    first warmup."""
+    spent, got = {}, None
+    for i in range(warmup + steps):
+        marks = [("start", torch.cuda.Event(enable_timing=True))]
+        marks[0][1].record()
+
+        def mark(name):
+            marks.append((name, torch.cuda.Event(enable_timing=True)))
+            marks[-1][1].record()
+
+        got = step(mark)
+        torch.cuda.synchronize()
+        if i >= warmup:
+            one = {}
+            for (_, a), (name, b) in zip(marks, marks[1:]):
+                one[name] = one.get(name, 0.0) + a.elapsed_time(b) * 1e6
+            for name, t in one.items():
+                spent.setdefault(name, []).append(t)
+    return got, {name: sorted(v)[len(v) // 2] for name, v in spent.items()}
+
+
 def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=100 * 10**9, seed=0):
     """Time the MoE layer ``layer`` (the first, if None) of a problem's model on the current device.
 
     Where all its experts do not fit ``limit_bytes``, an equal part of them takes an equal part of the tokens and
-    the expert and router times count for the whole.  Returns ns of the parts for one micro-batch, forward and
-    backward, the optimizer's ns a parameter and the router's counts."""
+    the times of the experts and of the rows' sum count for the whole; the router, whose work is tokens times experts,
+    then runs by itself at its whole size (by equal parts of its experts, where they are more than it takes).  Returns
+    ns of the parts for one micro-batch, forward and backward, the optimizer's ns a parameter and the router's counts."""
     m = problem["model"]
     moe = [i for i in range(m["n_layers"]) if m["is_moe"][i]]
     if not moe:
@@ -123,28 +170,16 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
             experts % (2 * part) == 0 and experts // (2 * part) >= top_k and tokens % (2 * part) == 0:
         part *= 2
     run = Layer(tokens // part, hidden, width, experts // part, top_k, state_bits, seed=seed)
-    spent = {}
-    got = None
-    for i in range(warmup + steps):
-        marks = [("start", torch.cuda.Event(enable_timing=True))]
-        marks[0][1].record()
-
-        def mark(name):
-            marks.append((name, torch.cuda.Event(enable_timing=True)))
-            marks[-1][1].record()
-
-        got = run.step(mark)
-        torch.cuda.synchronize()
-        if i >= warmup:
-            one = {}
-            for (_, a), (name, b) in zip(marks, marks[1:]):
-                one[name] = one.get(name, 0.0) + a.elapsed_time(b) * 1e6
-            for name, ns in one.items():
-                spent.setdefault(name, []).append(ns)
-    ns = {name: sorted(v)[len(v) // 2] for name, v in spent.items()}
+    got, ns = _times(run.step, warmup, steps)
+    route_ns = ns["route"]
+    if part > 1:
+        cut = 1   # where the router cannot take all experts at once
+        while experts // cut > operators.MAX_EXPERTS:
+            cut *= 2
+        route_ns = _times(_router_step(tokens, hidden, experts // cut, top_k, seed), warmup, steps)[1]["route"] * cut
     params = experts // part * 3 * width * hidden
     return {"layer": layer, "tokens": tokens, "hidden": hidden, "width": width, "experts": experts, "part": part,
-            "route_ns": ns["route"] * part, "combine_ns": ns["combine"] * part, "experts_ns": ns["experts"] * part,
+            "route_ns": route_ns, "combine_ns": ns["combine"] * part, "experts_ns": ns["experts"] * part,
             "opt_ns_per_param": ns["optimizer"] / params,
             "expert_tokens": got["routing"].count.cpu().numpy().astype(np.int64)}
 
