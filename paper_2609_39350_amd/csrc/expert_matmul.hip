@@ -14,9 +14,9 @@
 // Few rows an expert: bound by the reading of w.  16 tokens, 8 of 64 experts of 4,096
 // x 2,048: 156 us, 6.9 TB/s.  Many: bound by the products (MFMA busy 52 to 66 % of the
 // cycles) and by whole rounds of tiles over 256 CUs.  32,768 rows: 64 uneven experts
-// of 4,096 x 2,048 530 us, 1,040 TFLOP/s; 16 of 8,192 x 4,096 y 1,858, d_x 1,889, d_w
-// 2,172 us, 1,184, 1,164 and 1,012 TFLOP/s, where one library product of 8,192^3 reaches
-// 1,233 to 1,400.
+// of 4,096 x 2,048 530 to 540 us by the card, 1,020 to 1,040 TFLOP/s; 16 of 8,192 x 4,096
+// y 1,858 to 1,869, d_x 1,889 to 1,920, d_w 2,172 to 2,250 us, down to 1,176, 1,145 and 977
+// TFLOP/s, where one library product of 8,192^3 reaches 1,233 to 1,418.
 #include <type_traits>
 
 #include "operators.h"
