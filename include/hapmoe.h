@@ -610,6 +610,95 @@ int32_t hapmoe_adamw(const hapmoe_adamw_tensor *tensors, const void *const *grad
 int32_t hapmoe_adamw_moments(const hapmoe_adamw_tensor *tensors, void *const *d_m, void *const *d_v, int32_t n_tensors,
                              int32_t out_type, void *stream);
 
+/* ------------------------------------------------- around the layer
+ * Rows of x, d_y, d_out, add, the residual and the table are `..stride` elements apart;
+ * outputs are contiguous. */
+
+enum { HAPMOE_SOFTMAX = 0, HAPMOE_SIGMOID = 1 };
+#define HAPMOE_MAX_GROUPS 64     /* groups of experts of a balanced router */
+
+/* Router with a balanced choice.  Scores s of a token's logits x: sigmoid(x),
+ * or exp(x - max) over its sum over all experts.  The choice goes by c = s +
+ * bias[experts] (fp32; d_bias may be NULL, then by the logits' own order), as
+ * 64 bits resolve it: experts are `groups` runs of experts / groups; a group's
+ * score is the sum of the group_best (1 or 2) largest c in it, and the
+ * top_groups best groups stay, ties to the lowest; of their experts the top_k
+ * of the largest c, ties to the lowest, in descending order.  A weight is
+ * scale * s, or if renormalize scale * s over the sum of the chosen's s.  A
+ * NaN or -inf logit closes an expert to the token, a bias of NaN or -inf closes
+ * it to the choice; a group without an open expert is never chosen, and one
+ * with less than group_best counts those it has.  Where fewer than top_k
+ * experts are left the others are -1 with weight 0.  keep, the outputs, the
+ * order of the rows and the workspace as of hapmoe_route.  groups divides
+ * experts; scale > 0. */
+int32_t hapmoe_route_balanced(const void *d_logits, int32_t type, int64_t stride, int64_t tokens, int32_t experts,
+                              int32_t top_k, const float *d_bias, int32_t scores, int32_t groups, int32_t top_groups,
+                              int32_t group_best, const uint8_t *d_keep, int32_t renormalize, float scale,
+                              float *d_weight, int32_t *d_expert, int32_t *d_count, int32_t *d_offset, int32_t *d_slot,
+                              int32_t *d_place, void *d_ws, int64_t ws_bytes, void *stream);
+
+/* Gradient of its weights: d_d_logits [tokens][experts] of the logits' type,
+ * from what the forward call wrote and the same scores, keep, renormalize and
+ * scale.  The choice, and with it the bias and the groups, has none. */
+int32_t hapmoe_route_balanced_backward(const void *d_logits, int32_t type, int64_t stride, int64_t tokens,
+                                       int32_t experts, int32_t top_k, int32_t scores, const uint8_t *d_keep,
+                                       int32_t renormalize, float scale, const int32_t *d_expert, const float *d_weight,
+                                       const float *d_d_weight, void *d_d_logits, void *stream);
+
+/* Layer norm: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(mean of (x -
+ * mean)^2 + eps), for rows of `hidden` elements (at most 2^24).  d_mean NULL:
+ * not centred, mean is 0 (root mean square norm).  d_mean and d_rstd [rows]
+ * fp32 are what the gradient reads.  weight and bias [hidden] are of
+ * weight_type, `type` or F32; d_bias may be NULL.  eps >= 0. */
+int32_t hapmoe_layer_norm(const void *d_x, int32_t type, int64_t x_stride, int64_t rows, int64_t hidden,
+                          const void *d_weight, const void *d_bias, int32_t weight_type, float eps, float *d_mean,
+                          float *d_rstd, void *d_y, void *stream);
+
+/* Workspace of its gradient. */
+int32_t hapmoe_layer_norm_ws_bytes(int64_t rows, int64_t hidden, int64_t *bytes);
+
+/* Its gradients: with xhat = (x - mean) rstd and g = d_y weight, d_d_x = rstd
+ * (g - mean(g) - xhat mean(g xhat)) + add, rounded once (d_mean NULL: without
+ * mean(g); d_add may be NULL: the gradient that reaches x by a residual), and
+ * the sums over rows d_d_weight = sum d_y xhat, d_d_bias = sum d_y, [hidden]
+ * fp32 (d_d_bias may be NULL).  The order of the sums is fixed. */
+int32_t hapmoe_layer_norm_backward(const void *d_d_y, int64_t d_y_stride, const void *d_x, int32_t type,
+                                   int64_t x_stride, int64_t rows, int64_t hidden, const void *d_weight,
+                                   int32_t weight_type, const float *d_mean, const float *d_rstd, const void *d_add,
+                                   int64_t add_stride, void *d_d_x, float *d_d_weight, float *d_d_bias, void *d_ws,
+                                   int64_t ws_bytes, void *stream);
+
+/* out[t] = scale table[token[t]], [tokens][hidden] of the table's type; a token
+ * that is none of 0 .. vocab - 1 gives a row of zeros.  token_bits: 32 or 64,
+ * of the tokens' type (signed).  hidden <= 2^24. */
+int32_t hapmoe_embed(const void *d_token, int32_t token_bits, int64_t tokens, const void *d_table, int32_t type,
+                     int64_t stride, int64_t vocab, int64_t hidden, float scale, void *d_out, void *stream);
+
+/* Workspace of its gradient. */
+int32_t hapmoe_embed_ws_bytes(int64_t tokens, int64_t hidden, int64_t *bytes);
+
+/* The table's gradient, fp32: row v = scale * sum of d_out[t] over the t with
+ * token[t] = v.  add = 0: d_d_table [vocab][hidden] is written whole, rows
+ * without a token 0; else it is added to d_d_table, rows without a token are
+ * left as they are.  Each row's order of the sum is fixed. */
+int32_t hapmoe_embed_backward(const void *d_d_out, int32_t type, int64_t stride, int64_t tokens, int64_t hidden,
+                              const void *d_token, int32_t token_bits, int64_t vocab, float scale, int32_t add,
+                              float *d_d_table, void *d_ws, int64_t ws_bytes, void *stream);
+
+/* out = residual + x / (1 - q) where an element is kept, residual where it is
+ * not (0, whatever x is there); d_residual may be NULL.  The gradient of x is
+ * the same call of the gradient of out, without residual; that of residual is
+ * the gradient of out.  q is p rounded to a multiple of 2^-16.  Which are kept
+ * is a function of (seed, offset + *d_counter, index = row * columns + column)
+ * and of nothing else: Philox4x32-10 under the key seed of the counter words
+ * (index / 8 low, high, offset low, high) gives 8 numbers of 16 bits, the low
+ * half of a word before the high one; element index % 8 is kept where its
+ * number is at least q * 2^16.  d_counter (int64, may be NULL) is read when the
+ * call runs, so that a captured call drops others at every replay. */
+int32_t hapmoe_dropout(const void *d_x, int32_t type, int64_t x_stride, int64_t rows, int64_t columns,
+                       const void *d_residual, int64_t residual_stride, double p, uint64_t seed, uint64_t offset,
+                       const int64_t *d_counter, void *d_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

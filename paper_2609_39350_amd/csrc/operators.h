@@ -55,6 +55,55 @@ hipError_t launch_expert_matmul(const ExpertProduct &a, hipStream_t s);
 hipError_t launch_expert_matmul_grad_x(const ExpertProduct &a, hipStream_t s);
 hipError_t launch_expert_matmul_grad_w(const ExpertProduct &a, hipStream_t s);
 
+// The router with a balanced choice; ws as of launch_route.
+struct BalancedRoute {
+    const void *logits;
+    const float *bias;        // [experts] or null
+    const uint8_t *keep;      // [tokens] or null
+    float *weight;
+    int32_t *expert, *count, *offset, *slot, *place;
+    void *ws;
+    int64_t stride, tokens;
+    int type, experts, top_k, groups, top_groups, group_best;
+    float scale;
+    bool sigmoid, renormalize;
+};
+hipError_t launch_route_balanced(const BalancedRoute &a, hipStream_t s);
+hipError_t launch_route_balanced_backward(const void *logits, int type, int64_t stride, int64_t tokens, int experts,
+                                          int top_k, bool sigmoid, const uint8_t *keep, bool renormalize, float scale,
+                                          const int32_t *expert, const float *weight, const float *d_weight,
+                                          void *d_logits, hipStream_t s);
+
+struct LayerNorm {
+    const void *x;            // [rows][hidden], x_stride apart
+    const void *weight;       // [hidden]
+    const void *bias;         // [hidden] or null; forward
+    const void *d_y;          // backward
+    const void *add;          // backward: [rows][hidden] or null
+    void *out;                // y, or d_x
+    float *mean, *rstd;       // [rows]; mean null: not centred
+    float *d_weight, *d_bias; // backward; d_bias may be null
+    void *ws;
+    int64_t x_stride, d_y_stride, add_stride, rows, hidden;
+    int type, weight_type;
+    float eps;
+};
+hipError_t launch_layer_norm(const LayerNorm &a, hipStream_t s);
+int64_t layer_norm_ws_bytes(int64_t rows, int64_t hidden);
+hipError_t launch_layer_norm_backward(const LayerNorm &a, hipStream_t s);
+
+// token: int32, or int64 where wide
+hipError_t launch_embed(const void *token, bool wide, int64_t tokens, const void *table, int type, int64_t stride,
+                        int64_t vocab, int64_t hidden, float scale, void *out, hipStream_t s);
+int64_t embed_ws_bytes(int64_t tokens, int64_t hidden);
+hipError_t launch_embed_backward(const void *d_out, int type, int64_t stride, int64_t tokens, int64_t hidden,
+                                 const void *token, bool wide, int64_t vocab, float scale, bool add, float *d_table,
+                                 void *ws, hipStream_t s);
+
+hipError_t launch_dropout(const void *x, int type, int64_t x_stride, int64_t rows, int64_t columns,
+                          const void *residual, int64_t residual_stride, double p, uint64_t seed, uint64_t offset,
+                          const int64_t *counter, void *out, hipStream_t s);
+
 hipError_t launch_adamw(const hapmoe_adamw_tensor *t, const void *const *grads, int n, const hapmoe_adamw_args &a,
                         hipStream_t s);
 hipError_t launch_adamw_moments(const hapmoe_adamw_tensor *t, void *const *out_m, void *const *out_v, int n,

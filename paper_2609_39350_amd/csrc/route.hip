@@ -18,165 +18,14 @@
 // 32,768 tokens, 256 fp32 logits, top 8: choices 16.6 us (instruction issue; 7 of
 // them would be the reading; 21.4 with all keys in registers), the groups' sums 4.7,
 // the order 6.9, the gradient 12.4 (its 67 MB at 5.4 TB/s).  4 tokens of 64: 4.7 us.
-#include "operators.h"
+#include "router.h"
 
 namespace hapmoe {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPass = kThreads / 16;   // tokens of a workgroup of the gradient
-// Up to this many tokens one launch: us by one, by three: 8 experts, top 2: 64 tokens 6.0, 9.3, 128 7.9, 9.3; 256 experts, top
-// 8: 64 tokens 9.6, 12.4, 128 15.3, 14.0, 256 26.7, 14.2.
-constexpr int kOneLaunch = 64;
 constexpr int kPlaceRows = 1024;       // rows of a workgroup of the last kernel
-
-// Tokens of a workgroup.  us by 32, by 64: 256 experts, top 8: 16,384 tokens 18.7, 19.6, 32,768 25.9, 24.5, 65,536 38.6, 34.0;
-// 8 experts 13.8, 13.9, 15.7, 15.3, 21.7, 18.4; 1,024 experts, top 4, 32,768 tokens 49, 58.
-__host__ __device__ inline int group_tokens(int64_t tokens) { return tokens <= 64 * 512 ? 32 : 64; }
-
-// Neighbouring elements of a lane: those that it loads and stores at once where vectors are aligned; where they are not
-// it has the same, so that sums have the same order.
-template <typename T, int PER>
-constexpr int kStep = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER;
-template <typename T, int N>
-struct alignas(N * sizeof(T)) Piece {
-    T x[N];
-};
-// The expert whose logit is a lane's c-th: lanes take turns at steps of a row, so that loads and stores are whole lines, or
-// each has a RUN of PER, for the lowest of equal logits.
-template <int STEP, int PER, bool RUN>
-__device__ inline int expert_at(int lane, int c)
-{
-    return RUN ? lane * PER + c : (c / STEP * 16 + lane) * STEP + c % STEP;
-}
-
-// A token's logits in the registers of 16 lanes; closed experts (-inf, NaN, past the end, keep = 0) are -inf.
-template <typename T, int PER, bool VEC, bool RUN>
-__device__ inline void load_logits(float *v, const T *__restrict__ row, int lane, int experts, bool keep)
-{
-    constexpr int kN = kStep<T, PER>;
-#pragma unroll
-    for (int c = 0; c < PER; c += kN) {
-        const int e = expert_at<kN, PER, RUN>(lane, c);
-        if constexpr (VEC) {
-            const auto p = *reinterpret_cast<const Piece<T, kN> *>(row + e);
-#pragma unroll
-            for (int i = 0; i < kN; ++i) v[c + i] = to_f32(p.x[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kN; ++i) v[c + i] = e + i < experts ? to_f32(row[e + i]) : -INFINITY;
-        }
-    }
-#pragma unroll
-    for (int c = 0; c < PER; ++c) v[c] = keep && v[c] > -INFINITY ? v[c] : -INFINITY;
-}
-
-// threads of the first kernel: 32 KB of keys where they are in LDS, so that four workgroups share a CU
-constexpr int choose_threads(int per) { return per <= 16 ? 512 : 8192 / per; }
-// Where a lane's keys are in LDS too.  Taking a choice out of registers costs every lane a look at all of its PER keys,
-// three times; out of LDS the 16 lanes look at the chosen lane's keys together, once.
-constexpr bool keys_in_lds(int per) { return per >= 16; }
-constexpr int key_row(int per) { return 16 * per + 16; }   // a token's keys, the tokens' banks shifted
-
-// exp(x - top), 1 where x is the largest: also where both are infinite.  2^t with t = x log2(e) in two parts, so that the
-// error is that of the instruction (one unit) and not t's rounding; 0 below 2^-126.
-__device__ inline float exp_from(float x, float top)
-{
-    const float d = fmaxf(x - top, -200.0f);
-    const float t = d * 1.44269504f, rest = __builtin_fmaf(d, 1.92596303e-8f, __builtin_fmaf(d, 1.44269504f, -t));
-    const float y = __builtin_amdgcn_exp2f(t);
-    return x == top ? 1.0f : __builtin_fmaf(y, rest * 0.693147181f, y);
-}
-
-// Logits as whole numbers of the same order (both zeros equal), kClosed below all of them: the maxima need no care for
-// NaN, and the lane rotations go into them.
-constexpr int kClosed = INT32_MIN;
-__device__ inline int key_of(float x)
-{
-    const int b = __builtin_bit_cast(int, x + 0.0f);
-    return x == -INFINITY ? kClosed : b ^ (b >> 31 & 0x7fffffff);
-}
-__device__ inline float logit_of(int key) { return __builtin_bit_cast(float, key ^ (key >> 31 & 0x7fffffff)); }
-
-// v to exp(v - top), 0 where closed (top is not), and their sum
-template <int PER>
-__device__ inline float softmax(float *v, float top)
-{
-    float s = 0.0f;
-#pragma unroll
-    for (int c = 0; c < PER; ++c) s += v[c] = exp_from(v[c], top);
-    return row_reduce(s, Sum());
-}
-
-template <typename V, int PER>
-__device__ inline V lane_largest(const V *v)
-{
-    V m = v[0];
-#pragma unroll
-    for (int c = 1; c < PER; ++c) m = Max()(m, v[c]);
-    return m;
-}
-
-// The lowest lane of this lane's row of 16 where yes; 31 if none.
-__device__ inline int first_of_row(bool yes)
-{
-    return __ffs((int)((uint32_t)(__ballot(yes) >> (threadIdx.x & 48)) & 0xffff) | INT32_MIN) - 1;
-}
-
-// LDS written by lanes of a wave and read by others of it: its accesses are done in order, the compiler has to keep it.
-__device__ inline void wave_order()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
-// For each lane the lanes of the wave whose `key` is the same; bits: of the keys.
-__device__ inline uint64_t same_key(int key, int bits)
-{
-    uint64_t same = ~0ull;
-    for (int b = 0; b < bits; ++b) {
-        const uint64_t on = __ballot((key >> b) & 1);
-        same &= (key >> b) & 1 ? on : ~on;
-    }
-    return same;
-}
-
-// Exclusive sums over count[0 .. experts) by the workgroup, in place; returns the total.  sh: one int a wave.
-template <int THREADS>
-__device__ inline int scan_counts(int *count, int experts, int *sh)
-{
-    constexpr int kPer = HAPMOE_MAX_EXPERTS / THREADS;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int own[kPer], sum = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int e = threadIdx.x * kPer + i;
-        own[i] = e < experts ? count[e] : 0;
-        sum += own[i];
-    }
-    int inc = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(inc, d, 64);
-        if (lane >= d) inc += o;
-    }
-    if (lane == 63) sh[wave] = inc;
-    __syncthreads();
-    int before = inc - sum, total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        before += w < wave ? sh[w] : 0;
-        total += sh[w];
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int e = threadIdx.x * kPer + i;
-        if (e < experts) count[e] = before;
-        before += own[i];
-    }
-    __syncthreads();
-    return total;
-}
 
 // Choices, weights and ranks.  ALONE: the only workgroup, which finishes the order too; else rank goes to `place` and
 // the workgroup's counts to hist[workgroup][experts].
@@ -275,59 +124,7 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose(
         for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
     }
     __syncthreads();
-    // each wave ranks a run of the rows among its own
-    const int rows = here * top_k, run = (rows + kChoose - 1) / kChoose * 64;
-    const int wave = threadIdx.x >> 6, wave_lane = threadIdx.x & 63;
-    const int lo = min(wave * run, rows), hi = min(lo + run, rows);
-    int *const own = sums + wave * experts;
-    int32_t *const mine = place + first * top_k;
-    for (int r0 = lo; r0 < hi; r0 += 64) {
-        const int r = r0 + wave_lane;
-        const int e = r < hi ? chosen[r] : -1;
-        const uint64_t same = same_key(e + 1, bits);
-        const uint64_t below = same & ((1ull << wave_lane) - 1);
-        if (e >= 0) chosen[r] = (own[e] + __popcll(below)) << 10 | e;   // rank < 2^11, e < 2^10
-        // the counts before this round are read by every lane before the lowest of each expert adds to them
-        wave_order();
-        if (e >= 0 && below == 0) own[e] += __popcll(same);
-        wave_order();
-    }
-    __syncthreads();
-    // the counts of the waves before, and the whole
-    for (int e = threadIdx.x; e < experts; e += kChoose) {
-        int before = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const int n = sums[w * experts + e];
-            sums[w * experts + e] = before;
-            before += n;
-        }
-        if constexpr (ALONE)
-            count[e] = before;
-        else
-            hist[workgroup() * experts + e] = before;
-    }
-    __syncthreads();
-    if constexpr (ALONE) {
-        int *const at = sums + kWaves * experts;
-        for (int e = threadIdx.x; e < experts; e += kChoose) at[e] = count[e];
-        __syncthreads();
-        const int total = scan_counts<kChoose>(at, experts, sh);
-        for (int e = threadIdx.x; e < experts; e += kChoose) offset[e] = at[e];
-        if (threadIdx.x == 0) offset[experts] = total;
-        for (int r = threadIdx.x; r < rows; r += kChoose) {
-            const int c = chosen[r], e = c & 1023;
-            const int p = c < 0 ? -1 : at[e] + sums[r / run * experts + e] + (c >> 10);
-            place[r] = p;
-            if (p >= 0) slot[p] = r;
-            if (r >= total) slot[r] = -1;
-        }
-    } else {
-        for (int r = threadIdx.x; r < rows; r += kChoose) {
-            const int c = chosen[r];
-            mine[r] = c < 0 ? -1 : sums[r / run * experts + (c & 1023)] + (c >> 10);
-        }
-    }
+    order_rows<kChoose, ALONE>(chosen, sums, sh, here, top_k, first, experts, bits, place, hist, count, offset, slot);
 }
 
 // hist[group][experts] -> the sums over the groups before, and count.  A workgroup takes 16 experts, 16 lanes an equal
@@ -410,11 +207,13 @@ __global__ __launch_bounds__(kThreads) void k_place(const int32_t *__restrict__ 
 
 // d_logits.  Over all experts d_i = p_i (g_i - sum_j g_j w_j), g 0 for experts not chosen: p again from the logits.
 // Renormalised: w_j (g_j - sum g w) at the chosen, 0 elsewhere, and the logits are not read.
-template <typename T, int PER, bool VEC>
+// BALANCED: weights that were multiplied by a scale (the renormalised form's sum is over it), and where the scores are
+// sigmoids w_j (g_j - the same sum, if renormalised) (1 - s_j) at the chosen.
+template <typename T, int PER, bool VEC, bool BALANCED>
 __global__ __launch_bounds__(kThreads) void k_route_backward(
     const T *__restrict__ logits, int64_t stride, int64_t tokens, int experts, int top_k,
     const uint8_t *__restrict__ keep, int renormalize, const int32_t *__restrict__ expert,
-    const float *__restrict__ weight, const float *__restrict__ d_weight, T *__restrict__ d_logits)
+    const float *__restrict__ weight, const float *__restrict__ d_weight, T *__restrict__ d_logits, int sigmoid, float scale)
 {
     // what the chosen add, [token][16 lanes' PER + 1]: a lane's are a row of their own, a row's banks shifted by one
     __shared__ float added[kPass * 16 * (PER + 1)];
@@ -434,9 +233,10 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
         g[h] = who[h] >= 0 ? d_weight[t * top_k + j] : 0.0f;
         gw[h] = g[h] * w[h];
     }
-    const float mean = row_reduce(gw[0] + gw[1], Sum());
+    float mean = row_reduce(gw[0] + gw[1], Sum());
+    if constexpr (BALANCED) mean = renormalize ? mean / scale : sigmoid ? 0.0f : mean;
     float d[PER];
-    if (renormalize) {
+    if (renormalize || (BALANCED && sigmoid)) {
 #pragma unroll
         for (int c = 0; c < PER; ++c) d[c] = 0.0f;
     } else {
@@ -452,7 +252,12 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
     wave_order();
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        if (who[h] >= 0 && who[h] < 16 * PER) row[place_of(who[h])] = w[h] * (renormalize ? g[h] - mean : g[h]);
+        if (who[h] >= 0 && who[h] < 16 * PER) {
+            float add = w[h] * (renormalize ? g[h] - mean : g[h]);
+            if constexpr (BALANCED)
+                if (sigmoid) add = who[h] < experts ? add * sigmoid_of(-to_f32(logits[t * stride + who[h]])) : 0.0f;
+            row[place_of(who[h])] = add;
+        }
     wave_order();
 #pragma unroll
     for (int c = 0; c < PER; ++c) d[c] += mine[c];
@@ -473,24 +278,6 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
     }
 }
 
-// a call's PER for its experts, and whether whole vectors can be loaded
-template <typename F>
-hipError_t by_experts(int experts, F f)
-{
-    if (experts <= 64) return f(std::integral_constant<int, 4>());
-    if (experts <= 128) return f(std::integral_constant<int, 8>());
-    if (experts <= 256) return f(std::integral_constant<int, 16>());
-    if (experts <= 512) return f(std::integral_constant<int, 32>());
-    return f(std::integral_constant<int, 64>());
-}
-template <typename F>
-hipError_t by_type(int type, F f)
-{
-    if (type == HAPMOE_F32) return f(float());
-    if (type == HAPMOE_BF16) return f(bf16());
-    return f(f16());
-}
-
 }  // namespace
 
 int64_t route_ws_bytes(int64_t tokens, int experts, int top_k)
@@ -498,6 +285,19 @@ int64_t route_ws_bytes(int64_t tokens, int experts, int top_k)
     (void)top_k;
     if (tokens <= kOneLaunch) return 0;
     return ceil_div(tokens, group_tokens(tokens)) * experts * 4;
+}
+
+hipError_t launch_route_order(const int32_t *expert, int32_t *hist, int64_t groups, int64_t rows, int experts,
+                              int group_rows, int32_t *count, int32_t *offset, int32_t *place, int32_t *slot,
+                              hipStream_t s)
+{
+    hipLaunchKernelGGL(k_scan_groups, dim3((unsigned)ceil_div(experts, kScanExperts)), dim3(kScanThreads), 0, s, hist,
+                       (int)groups, experts, count);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_place, many(ceil_div(rows, kPlaceRows)), dim3(kThreads), 0, s, expert, hist, count,
+                       rows, experts, group_rows, offset, place, slot);
+    return hipGetLastError();
 }
 
 hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t tokens, int experts, int top_k,
@@ -528,18 +328,14 @@ hipError_t launch_route(const void *logits, int type, int64_t stride, int64_t to
         });
     });
     if (e != hipSuccess || alone) return e;
-    hipLaunchKernelGGL(k_scan_groups, dim3((unsigned)ceil_div(experts, kScanExperts)), dim3(kScanThreads), 0, s, hist,
-                       (int)groups, experts, count);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int64_t rows = tokens * top_k;
-    hipLaunchKernelGGL(k_place, many(ceil_div(rows, kPlaceRows)), dim3(kThreads), 0, s, expert, hist, count,
-                       rows, experts, group * top_k, offset, place, slot);
-    return hipGetLastError();
+    return launch_route_order(expert, hist, groups, tokens * top_k, experts, group * top_k, count, offset, place, slot, s);
 }
 
-hipError_t launch_route_backward(const void *logits, int type, int64_t stride, int64_t tokens, int experts, int top_k,
-                                 const uint8_t *keep, bool renormalize, const int32_t *expert, const float *weight,
-                                 const float *d_weight, void *d_logits, hipStream_t s)
+namespace {
+template <bool BALANCED>
+hipError_t route_backward(const void *logits, int type, int64_t stride, int64_t tokens, int experts, int top_k,
+                          const uint8_t *keep, bool renormalize, const int32_t *expert, const float *weight,
+                          const float *d_weight, void *d_logits, bool sigmoid, float scale, hipStream_t s)
 {
     return by_type(type, [&](auto t) {
         using T = decltype(t);
@@ -547,13 +343,32 @@ hipError_t launch_route_backward(const void *logits, int type, int64_t stride, i
             constexpr int PER = decltype(per)::value;
             const bool vec = experts == 16 * PER && aligned(logits, 16) && aligned(d_logits, 16) &&
                              stride * (int64_t)sizeof(T) % 16 == 0;
-            hipLaunchKernelGGL((vec ? k_route_backward<T, PER, true> : k_route_backward<T, PER, false>),
+            hipLaunchKernelGGL((vec ? k_route_backward<T, PER, true, BALANCED> : k_route_backward<T, PER, false, BALANCED>),
                                many(ceil_div(tokens, kPass)), dim3(kThreads), 0, s,
                                static_cast<const T *>(logits), stride, tokens, experts, top_k, keep,
-                               renormalize ? 1 : 0, expert, weight, d_weight, static_cast<T *>(d_logits));
+                               renormalize ? 1 : 0, expert, weight, d_weight, static_cast<T *>(d_logits),
+                               sigmoid ? 1 : 0, scale);
             return hipGetLastError();
         });
     });
+}
+}  // namespace
+
+hipError_t launch_route_backward(const void *logits, int type, int64_t stride, int64_t tokens, int experts, int top_k,
+                                 const uint8_t *keep, bool renormalize, const int32_t *expert, const float *weight,
+                                 const float *d_weight, void *d_logits, hipStream_t s)
+{
+    return route_backward<false>(logits, type, stride, tokens, experts, top_k, keep, renormalize, expert, weight,
+                                 d_weight, d_logits, false, 1.0f, s);
+}
+
+hipError_t launch_route_balanced_backward(const void *logits, int type, int64_t stride, int64_t tokens, int experts,
+                                          int top_k, bool sigmoid, const uint8_t *keep, bool renormalize, float scale,
+                                          const int32_t *expert, const float *weight, const float *d_weight,
+                                          void *d_logits, hipStream_t s)
+{
+    return route_backward<true>(logits, type, stride, tokens, experts, top_k, keep, renormalize, expert, weight,
+                                d_weight, d_logits, sigmoid, scale, s);
 }
 
 }  // namespace hapmoe

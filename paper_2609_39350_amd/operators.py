@@ -8,6 +8,13 @@ parameter -- are quantities of these operators:
   combine, combine_backward        a token's expert outputs put together
   AdamW                            the optimizer step, moments in 32 or 8 bits
 
+and what stands around the layer in a training step:
+
+  embed, embed_backward            the first stage's table, its gradient summed by token
+  layer_norm, .._backward          rows' norm with or without the mean, the weight's gradient over rows
+  route_balanced, .._backward      a router of scores, a bias for the choice and groups of experts
+  dropout, dropout_backward        by a counter-based generator, without a mask, onto a residual
+
 Thin calls of the C functions in include/hapmoe.h, which states each formula.  Tensors are on
 the current device; work is enqueued on its current stream and outputs are allocated there
 unless they are given.  A tensor, size or number that an operator cannot take raises ValueError
@@ -52,7 +59,7 @@ def _lib():
     global _LIB
     if _LIB is None:
         L = binding.lib()
-        i32, i64, vp = C.c_int32, C.c_int64, C.c_void_p
+        i32, i64, vp, f32 = C.c_int32, C.c_int64, C.c_void_p, C.c_float
         for name, args in {
                 "hapmoe_route_ws_bytes": [i64, i32, i32, C.POINTER(i64)],
                 "hapmoe_route": [vp, i32, i64, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp],
@@ -63,6 +70,17 @@ def _lib():
                 "hapmoe_expert_matmul_grad_x": [vp, i64, vp, i32, i64, i32, i64, i64, vp, vp, vp],
                 "hapmoe_expert_matmul_grad_w": [vp, i64, vp, i64, i64, i32, i64, i32, i64, i64, vp, vp, i32, i32, vp,
                                                 vp],
+                "hapmoe_route_balanced": [vp, i32, i64, i64, i32, i32, vp, i32, i32, i32, i32, vp, i32, f32, vp, vp, vp, vp,
+                                          vp, vp, vp, i64, vp],
+                "hapmoe_route_balanced_backward": [vp, i32, i64, i64, i32, i32, i32, vp, i32, f32, vp, vp, vp, vp, vp],
+                "hapmoe_layer_norm": [vp, i32, i64, i64, i64, vp, vp, i32, f32, vp, vp, vp, vp],
+                "hapmoe_layer_norm_ws_bytes": [i64, i64, C.POINTER(i64)],
+                "hapmoe_layer_norm_backward": [vp, i64, vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, i64, vp, vp, vp, vp,
+                                               i64, vp],
+                "hapmoe_embed": [vp, i32, i64, vp, i32, i64, i64, i64, f32, vp, vp],
+                "hapmoe_embed_ws_bytes": [i64, i64, C.POINTER(i64)],
+                "hapmoe_embed_backward": [vp, i32, i64, i64, i64, vp, i32, i64, f32, i32, vp, vp, i64, vp],
+                "hapmoe_dropout": [vp, i32, i64, i64, i64, vp, i64, C.c_double, C.c_uint64, C.c_uint64, vp, vp, vp],
                 "hapmoe_adamw": [C.POINTER(_Tensor), vp, i32, C.POINTER(_Args), vp],
                 "hapmoe_adamw_moments": [C.POINTER(_Tensor), vp, vp, i32, i32, vp]}.items():
             f = getattr(L, name)
@@ -215,6 +233,63 @@ def route_backward(logits, routing: Routing, d_weight, keep=None, renormalize=Tr
     return d_logits
 
 
+SCORES = {"softmax": 0, "sigmoid": 1}
+MAX_GROUPS = 64
+
+
+def route_balanced(logits, top_k: int, bias=None, scores="sigmoid", groups=1, top_groups=None, group_best=2, keep=None,
+                   renormalize=True, scale=1.0, out: Routing = None) -> Routing:
+    """The top_k experts of every row of ``logits`` [tokens, experts] by their score ("sigmoid" or "softmax") plus
+    ``bias`` [experts] fp32, out of the ``top_groups`` of ``groups`` equal groups of experts whose ``group_best`` (1 or
+    2) best add up to most; weights are the scores without the bias, times ``scale`` (``hapmoe_route_balanced``).
+    top_groups: None: all groups.  keep, renormalize and out as in ``route``."""
+    stride = _matrix("logits", logits, _TYPES)
+    tokens, experts = logits.shape
+    kind = _scores(scores)
+    top_groups = groups if top_groups is None else top_groups
+    if not 1 <= groups <= MAX_GROUPS or experts % groups or not 1 <= top_groups <= groups or group_best not in (1, 2):
+        raise ValueError(f"no choice of {group_best} of {top_groups} of {groups} groups of {experts} experts")
+    if bias is not None:
+        _array("bias", bias, torch.float32, experts)
+    if out is None:
+        out = Routing(tokens, experts, top_k, logits.device)
+    else:
+        _need((out.tokens, out.experts, out.top_k) == (tokens, experts, top_k) and
+              out.expert.device == logits.device, "out: made for other sizes or another device")
+        _need(out._addresses() == out._outputs, "out: a buffer was replaced")
+    _check(_lib().hapmoe_route_balanced(logits.data_ptr(), _TYPES[logits.dtype], stride, tokens, experts, top_k,
+                                        None if bias is None else bias.data_ptr(), kind, groups, top_groups, group_best,
+                                        _keep(keep, tokens), 1 if renormalize else 0, scale, *out._outputs,
+                                        out._ws_bytes, _stream(logits)), "hapmoe_route_balanced")
+    return out
+
+
+def _scores(scores):
+    kind = SCORES.get(scores) if isinstance(scores, str) else None
+    if kind is None:
+        raise ValueError(f"scores: one of {', '.join(SCORES)}, not {scores}")
+    return kind
+
+
+def route_balanced_backward(logits, routing: Routing, d_weight, scores="sigmoid", keep=None, renormalize=True, scale=1.0):
+    """The gradient of the logits from that of the weights [tokens, top_k] fp32
+    (``hapmoe_route_balanced_backward``), with the forward call's routing, scores, keep, renormalize and scale."""
+    stride = _matrix("logits", logits, _TYPES)
+    tokens, experts = logits.shape
+    kind = _scores(scores)
+    _need((routing.tokens, routing.experts) == (tokens, experts), "routing: made for other sizes")
+    k = routing.top_k
+    _array("routing.expert", routing.expert, torch.int32, tokens, k)
+    _array("routing.weight", routing.weight, torch.float32, tokens, k)
+    _array("d_weight", d_weight, torch.float32, tokens, k)
+    d_logits = logits.new_empty((tokens, experts))
+    _check(_lib().hapmoe_route_balanced_backward(
+        logits.data_ptr(), _TYPES[logits.dtype], stride, tokens, experts, k, kind, _keep(keep, tokens),
+        1 if renormalize else 0, scale, routing.expert.data_ptr(), routing.weight.data_ptr(), d_weight.data_ptr(),
+        d_logits.data_ptr(), _stream(logits)), "hapmoe_route_balanced_backward")
+    return d_logits
+
+
 # --------------------------------------------------- a token's expert outputs
 def _rows(name, t):
     if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _TYPES and t.dim() == 2 and t.shape[1] \
@@ -336,6 +411,135 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
                                               None if slot is None else slot.data_ptr(), top_k, _TYPES[dtype],
                                               d_w.data_ptr(), _stream(x)), "hapmoe_expert_matmul_grad_w")
     return d_w
+
+
+# ----------------------------------------------------------- around the layer
+def _vector(name, t, types, n):
+    """A contiguous vector of n elements of one of the types."""
+    _on_device(name, t)
+    if t.dtype not in types:
+        raise ValueError(f"{name}: one of {', '.join(str(x) for x in types)}, not {t.dtype}")
+    _array(name, t, t.dtype, n)
+
+
+def layer_norm(x, weight, bias=None, eps=1e-5, center=True):
+    """y = (x - mean) * rstd * weight + bias of the rows of ``x`` [rows, hidden] (``hapmoe_layer_norm``), and mean and
+    rstd [rows] fp32, which ``layer_norm_backward`` takes.  center False: mean counts as 0 (root mean square norm) and
+    is None.  weight and bias [hidden]: fp32 or x's type, both the same."""
+    stride = _matrix("x", x, _TYPES)
+    rows, hidden = x.shape
+    _vector("weight", weight, (torch.float32, x.dtype), hidden)
+    if bias is not None:
+        _array("bias", bias, weight.dtype, hidden)
+    y = x.new_empty((rows, hidden))
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    mean = torch.empty_like(rstd) if center else None
+    _check(_lib().hapmoe_layer_norm(x.data_ptr(), _TYPES[x.dtype], stride, rows, hidden, weight.data_ptr(),
+                                    None if bias is None else bias.data_ptr(), _TYPES[weight.dtype], eps,
+                                    None if mean is None else mean.data_ptr(), rstd.data_ptr(), y.data_ptr(),
+                                    _stream(x)), "hapmoe_layer_norm")
+    return y, mean, rstd
+
+
+def layer_norm_backward(d_y, x, weight, mean, rstd, add=None, bias=True):
+    """The gradients (d_x, d_weight [hidden] fp32, d_bias [hidden] fp32) of ``layer_norm`` from that of y
+    (``hapmoe_layer_norm_backward``); mean None: of the form that is not centred.  add [rows, hidden]: a gradient
+    that reaches x another way, added to d_x.  bias False: d_bias is None."""
+    stride = _matrix("x", x, _TYPES)
+    rows, hidden = x.shape
+    steps = []
+    for name, t in (("d_y", d_y), ("add", add)):
+        if t is None and name == "add":
+            steps.append(hidden)
+            continue
+        steps.append(_matrix(name, t, (x.dtype,)))
+        if t.shape != x.shape:
+            raise ValueError(f"{name}: shape {tuple(x.shape)}, not {tuple(t.shape)}")
+    _vector("weight", weight, (torch.float32, x.dtype), hidden)
+    _array("rstd", rstd, torch.float32, rows)
+    if mean is not None:
+        _array("mean", mean, torch.float32, rows)
+    need = C.c_int64(0)
+    _check(_lib().hapmoe_layer_norm_ws_bytes(rows, hidden, C.byref(need)), "hapmoe_layer_norm_ws_bytes")
+    d_x = x.new_empty((rows, hidden))
+    d_weight = torch.empty(hidden, dtype=torch.float32, device=x.device)
+    d_bias = torch.empty_like(d_weight) if bias else None
+    ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+    _check(_lib().hapmoe_layer_norm_backward(
+        d_y.data_ptr(), steps[0], x.data_ptr(), _TYPES[x.dtype], stride, rows, hidden, weight.data_ptr(),
+        _TYPES[weight.dtype], None if mean is None else mean.data_ptr(), rstd.data_ptr(),
+        None if add is None else add.data_ptr(), steps[1], d_x.data_ptr(), d_weight.data_ptr(),
+        None if d_bias is None else d_bias.data_ptr(), ws.data_ptr(), need.value, _stream(x)),
+        "hapmoe_layer_norm_backward")
+    return d_x, d_weight, d_bias
+
+
+_TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
+
+
+def embed(token, table, scale=1.0):
+    """out[t] = scale * table[token[t]] for ``token`` [tokens] int32 or int64 and ``table`` [vocab, hidden]
+    (``hapmoe_embed``); a token out of the table gives a row of zeros."""
+    stride = _matrix("table", table, _TYPES)
+    _vector("token", token, _TOKEN_BITS, None)
+    vocab, hidden = table.shape
+    out = table.new_empty((token.shape[0], hidden))
+    _check(_lib().hapmoe_embed(token.data_ptr(), _TOKEN_BITS[token.dtype], token.shape[0], table.data_ptr(),
+                               _TYPES[table.dtype], stride, vocab, hidden, scale, out.data_ptr(), _stream(table)),
+           "hapmoe_embed")
+    return out
+
+
+def embed_backward(d_out, token, vocab: int, scale=1.0, into=None):
+    """The gradient of ``embed``'s table [vocab, hidden] in fp32 from that of its result
+    (``hapmoe_embed_backward``).  into: an fp32 gradient of that shape that it is added to, which is returned; rows
+    without a token stay as they are.  Each row's sum has a fixed order."""
+    stride = _matrix("d_out", d_out, _TYPES)
+    tokens, hidden = d_out.shape
+    _vector("token", token, _TOKEN_BITS, tokens)
+    if not 1 <= vocab < 2**31:
+        raise ValueError(f"vocab: at least 1 and below 2^31, not {vocab}")
+    if into is None:
+        d_table = torch.empty((vocab, hidden), dtype=torch.float32, device=d_out.device)
+    else:
+        _array("into", into, torch.float32, vocab, hidden)
+        d_table = into
+    need = C.c_int64(0)
+    _check(_lib().hapmoe_embed_ws_bytes(tokens, hidden, C.byref(need)), "hapmoe_embed_ws_bytes")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=d_out.device)
+    _check(_lib().hapmoe_embed_backward(d_out.data_ptr(), _TYPES[d_out.dtype], stride, tokens, hidden, token.data_ptr(),
+                                        _TOKEN_BITS[token.dtype], vocab, scale, 0 if into is None else 1,
+                                        d_table.data_ptr(), ws.data_ptr(), need.value, _stream(d_out)),
+           "hapmoe_embed_backward")
+    return d_table
+
+
+def dropout(x, p, seed, offset=0, residual=None, counter=None):
+    """residual + x / (1 - p) where an element of ``x`` [rows, columns] is kept, residual (or 0) where it is dropped,
+    with a chance of p rounded to a multiple of 2^-16 (``hapmoe_dropout``).  Which are dropped is a function of seed,
+    offset and the element's index alone: give every dropout of a step another offset.  counter: an int64 tensor of
+    one element on the device that is added to offset when the call runs, for captured calls."""
+    stride = _matrix("x", x, _TYPES)
+    step = 0
+    if residual is not None:
+        step = _matrix("residual", residual, (x.dtype,))
+        if residual.shape != x.shape:
+            raise ValueError(f"residual: shape {tuple(x.shape)}, not {tuple(residual.shape)}")
+    if counter is not None:
+        _array("counter", counter, torch.int64, 1)
+    rows, columns = x.shape
+    out = x.new_empty((rows, columns))
+    _check(_lib().hapmoe_dropout(x.data_ptr(), _TYPES[x.dtype], stride, rows, columns,
+                                 None if residual is None else residual.data_ptr(), step, p, seed & (2**64 - 1),
+                                 offset & (2**64 - 1), None if counter is None else counter.data_ptr(), out.data_ptr(),
+                                 _stream(x)), "hapmoe_dropout")
+    return out
+
+
+def dropout_backward(d_out, p, seed, offset=0, counter=None):
+    """The gradient of ``dropout``'s x from that of its result, with the forward call's numbers; that of residual is
+    d_out."""
+    return dropout(d_out, p, seed, offset, None, counter)
 
 
 # -------------------------------------------------------------- the optimizer
