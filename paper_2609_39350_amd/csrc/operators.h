@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "hapmoe.h"
 
@@ -138,6 +139,51 @@ template <typename T>
 __device__ inline T from_f32(float x)
 {
     return (T)x;
+}
+
+// Eight neighbours of any alignment, as the words that hold them.
+template <typename T>
+using Words __attribute__((ext_vector_type(2 * sizeof(T)))) = uint32_t;
+template <typename T>
+__device__ inline Words<T> load_words(const T *p)
+{
+    Words<T> w;
+    __builtin_memcpy(&w, p, sizeof(w));
+    return w;
+}
+template <typename T>
+__device__ inline void store_words(T *p, const Words<T> &w)
+{
+    __builtin_memcpy(p, &w, sizeof(w));
+}
+template <typename T>
+__device__ inline float element(const Words<T> &w, int j)
+{
+    if constexpr (sizeof(T) == 4)
+        return __builtin_bit_cast(float, (uint32_t)w[j]);
+    else if constexpr (std::is_same<T, bf16>::value)
+        return __builtin_bit_cast(float, j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+    else
+        return (float)__builtin_bit_cast(f16, (uint16_t)(w[j / 2] >> j % 2 * 16));
+}
+// rounded to nearest even
+template <typename T>
+__device__ inline Words<T> words_of(const float *v)
+{
+    Words<T> w;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_bit_cast(uint32_t, v[j]);
+    } else {
+        typedef float F2 __attribute__((ext_vector_type(2)));
+        typedef T T2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const F2 two = {v[2 * j], v[2 * j + 1]};
+            w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, T2));
+        }
+    }
+    return w;
 }
 
 template <int CTRL>
