@@ -2,20 +2,22 @@
 //
 // out[t] = scale table[token[t]], a row of zeros where the token is none of the table's.
 //
-// The gradient's row of a token is the sum over its places in the order of t, with no atomics.  A workgroup sorts up to
-// 16,384 places by token in LDS: a stable counting sort, 9 bits of the token a pass; more places are several such
-// segments, whose sums follow each other.  Then workgroups take equal chunks of the sorted places, whatever the tokens' shares: a
-// token that lies within a chunk is written, one that goes on into the next leaves its sums in the workspace, and a last
-// launch puts those together.
+// The gradient's row of a token is the sum over its places in the order of t, with no atomics.  Workgroups sort up to
+// 4,096 places each by token in LDS: a stable counting sort, up to 9 bits of the token a pass; a launch puts up to 16
+// such segments into one order, every place by a search in each of the others.  Then workgroups take equal chunks of the
+// sorted places, whatever the tokens' shares: a token that lies within a chunk is written, one that goes on into the
+// next leaves its sums in the workspace, and a last launch puts those together.  Rows without a token are cleared by
+// further workgroups of the same launch, which look for them in the sorted places.
 #include "operators.h"
 
 namespace hapmoe {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSegment = 16384;    // places of a sort: tokens, two orders and counts in 144 KB of LDS
+constexpr int kSegment = 4096;     // places of a sort
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSteps = kSegment / kSortThreads;
 constexpr int kDigit = 9, kBins = 1 << kDigit;
+constexpr int kWays = 16;          // segments that a launch puts together
 
 template <typename I>
 __device__ inline int64_t token_at(const void *token, int64_t t)
@@ -23,26 +25,58 @@ __device__ inline int64_t token_at(const void *token, int64_t t)
     return (int64_t) static_cast<const I *>(token)[t];
 }
 
-template <typename T, typename I, bool VEC>
+// Eight columns of a thread; where less than eight are left, the row's last 8, of which the first `skip` are others'.
+struct Columns {
+    int first, skip;
+    __device__ Columns(int hidden, int k) : first(min(k * 8, hidden - 8)), skip(k * 8 - first) {}
+};
+
+template <typename T>
+__device__ inline void put(T *__restrict__ row, const Columns &c, const float *v)
+{
+    if (c.skip == 0) {
+        store_words(row + c.first, words_of<T>(v));
+    } else {
+#pragma unroll
+        for (int j = 1; j < 8; ++j)
+            if (j >= c.skip) row[c.first + j] = from_f32<T>(v[j]);
+    }
+}
+
+// Threads of a row (of 8 columns each): a power of two.
+__host__ __device__ inline int lanes_of(int64_t hidden)
+{
+    int lanes = 8;
+    while (lanes < kThreads && lanes * 8 < hidden) lanes *= 2;
+    return lanes;
+}
+
+// A row by `lanes` threads, or by one where it is shorter than a vector.  LANES: that number, 64 at least, so that a
+// wave's token and addresses are the same in every lane (32,768 of 4,096: 76 us, 89 with each lane's own), or 0.
+template <typename T, typename I, int LANES>
 __global__ __launch_bounds__(kThreads) void k_embed(const void *__restrict__ token, int64_t tokens,
                                                     const T *__restrict__ table, int64_t stride, int64_t vocab,
-                                                    int64_t hidden, float scale, T *__restrict__ out)
+                                                    int hidden, int lanes, float scale, T *__restrict__ out)
 {
-    const int64_t t = workgroup(), h = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * (VEC ? 8 : 1);
-    if (t >= tokens || h >= hidden) return;
+    if constexpr (LANES > 0) lanes = LANES;
+    const int in = threadIdx.x / lanes;
+    const int64_t t = workgroup() * (kThreads / lanes) + (LANES > 0 ? __builtin_amdgcn_readfirstlane(in) : in);
+    if (t >= tokens) return;
     const int64_t v = token_at<I>(token, t);
     const bool real = (uint64_t)v < (uint64_t)vocab;
-    if constexpr (VEC) {
-        Vec8<T> r = {};
-        if (real) {
-            r = *reinterpret_cast<const Vec8<T> *>(table + v * stride + h);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(to_f32(r.v[i]) * scale);
-        }
-        *reinterpret_cast<Vec8<T> *>(out + t * hidden + h) = r;
-    } else {
-        out[t * hidden + h] = from_f32<T>(real ? to_f32(table[v * stride + h]) * scale : 0.0f);
+    if (LANES == 0 && hidden < 8) {
+        for (int h = 0; h < hidden; ++h) out[t * hidden + h] = from_f32<T>(real ? to_f32(table[v * stride + h]) * scale : 0.0f);
+        return;
     }
+    const Columns c(hidden, blockIdx.y * lanes + threadIdx.x % lanes);
+    if (c.skip >= 8) return;
+    float r[8] = {};
+    if (real) {
+        const Words<T> w = load_words(table + v * stride + c.first);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = element<T>(w, j) * scale;
+    }
+    put(out + t * hidden, c, r);
 }
 
 // Segment blockIdx.x: sorted[i] = (token, place) for its places, the tokens ascending, the places of one ascending.
@@ -128,81 +162,246 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const void *__restrict__ 
     }
 }
 
-__global__ __launch_bounds__(kThreads) void k_zero(float *__restrict__ p, int64_t n)
+// Runs of `run` sorted places each -> runs of kWays * run: a place goes behind its own run's earlier ones and, of every
+// other run, those of lower tokens, and of the runs before its own those of the same token too.  A search begins in
+// kSamples places of each run, out of LDS: 17 us for 32,768 places with all of its steps out of the cache.
+constexpr int kSamples = 128;
+__global__ __launch_bounds__(kThreads) void k_merge(const int2 *__restrict__ from, int2 *__restrict__ to, int n, int run)
 {
-    const int64_t i = (workgroup() * kThreads + threadIdx.x) * 4;
-    if (i + 4 <= n && ((uintptr_t)p & 15) == 0) {
-        *reinterpret_cast<float4 *>(p + i) = make_float4(0, 0, 0, 0);
-    } else {
-        for (int64_t j = i; j < i + 4 && j < n; ++j) p[j] = 0.0f;
+    __shared__ int sample[kWays][kSamples];
+    const int64_t first = workgroup() * kThreads, whole = (int64_t)run * kWays;
+    if (first >= n) return;
+    const int64_t base = first / whole * whole;   // of all of this workgroup's places: kThreads divides a run
+    const int i = (int)min(first + threadIdx.x, (int64_t)n - 1), step = run / kSamples;
+    auto begin = [&](int w) { return (int)min(base + (int64_t)w * run, (int64_t)n); };
+    const int2 v = from[i];
+#pragma unroll
+    for (int q = 0; q < kWays * kSamples / kThreads; ++q) {
+        const int s = q * kThreads + threadIdx.x;
+        const int64_t at = base + (int64_t)s * step;
+        (&sample[0][0])[s] = at < n ? from[at].x : INT32_MAX;
     }
-}
-
-// A row of the gradient, or what is added to it.
-template <int N>
-__device__ inline void put(float *__restrict__ to, const float *sum, float scale, bool add)
-{
+    __syncthreads();
+    const int mine = i / run * run;
+    int lo[kWays], size[kWays];   // the first that goes behind v is in lo .. lo + size
 #pragma unroll
-    for (int i = 0; i < N; ++i) to[i] = (add ? to[i] : 0.0f) + sum[i] * scale;
-}
-
-// Chunk `workgroup` of a segment of n sorted places, N columns a thread.
-template <typename T, int N>
-__global__ __launch_bounds__(kThreads) void k_embed_sum(const T *__restrict__ d_out, int64_t stride, int64_t hidden,
-                                                        const int2 *__restrict__ sorted, int n, int chunk, int vocab,
-                                                        float scale, bool add, float *__restrict__ d_table,
-                                                        float *__restrict__ part)
-{
-    const int64_t h = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * N;
-    if (h >= hidden) return;
-    const int lo = blockIdx.x * chunk, hi = min(lo + chunk, n);
-    float sum[N] = {};
-    for (int i = lo; i < hi; ++i) {
-        const int2 at = sorted[i];
-        if (at.x == vocab) break;
-        const T *const row = d_out + at.y * stride + h;
+    for (int w = 0; w < kWays; ++w) {
+        const int key = begin(w) < mine ? v.x : v.x - 1;   // those up to it go before: tokens are whole numbers
+        int c = 0;   // samples that do
 #pragma unroll
-        for (int c = 0; c < N; ++c) sum[c] += to_f32(row[c]);
-        const bool goes_on = i + 1 < n && sorted[i + 1].x == at.x;
-        if (goes_on && i + 1 < hi) continue;
-        const bool began = lo > 0 && sorted[lo - 1].x == at.x;
-        if (began || goes_on) {
-            float *const to = part + ((int64_t)blockIdx.x * 2 + (began ? 0 : 1)) * hidden + h;
+        for (int half = kSamples / 2; half > 0; half >>= 1) c += sample[w][c + half - 1] <= key ? half : 0;
+        c += sample[w][c] <= key ? 1 : 0;
+        lo[w] = begin(w) + (c > 0 ? (c - 1) * step + 1 : 0);
+        size[w] = begin(w) == mine || c == 0 ? 0 : max(min(begin(w) + c * step, begin(w + 1)) - lo[w], 0);
+    }
+    for (int most = step; most > 0; most >>= 1) {   // all runs' searches side by side
+        int other[kWays];
 #pragma unroll
-            for (int c = 0; c < N; ++c) to[c] = sum[c];
-        } else {
-            put<N>(d_table + at.x * hidden + h, sum, scale, add);
+        for (int w = 0; w < kWays; ++w) other[w] = from[min(lo[w] + (size[w] >> 1), n - 1)].x;
+#pragma unroll
+        for (int w = 0; w < kWays; ++w) {
+            const int half = size[w] >> 1;
+            const bool before = size[w] > 0 && other[w] <= (begin(w) < mine ? v.x : v.x - 1);
+            size[w] = before ? size[w] - half - 1 : half;
+            lo[w] += before ? half + 1 : 0;
         }
+    }
+    int64_t at = base + (i - mine);
 #pragma unroll
-        for (int c = 0; c < N; ++c) sum[c] = 0.0f;
+    for (int w = 0; w < kWays; ++w)
+        if (begin(w) != mine) at += lo[w] - begin(w);
+    if (first + threadIdx.x < n) to[at] = v;
+}
+
+constexpr int kChunkMost = 128, kRowsAhead = 8;
+
+// The first `sums` workgroups of x have chunks of the n sorted places, the others rows to clear where they have no token.
+// ADD: no rows to clear; what a token's row holds is loaded with the rows that are added to it.
+template <typename T, bool ADD>
+__global__ __launch_bounds__(kThreads) void k_embed_sum(const T *__restrict__ d_out, int64_t stride, int hidden,
+                                                        const int2 *__restrict__ sorted, int64_t n, int chunk, int lanes,
+                                                        int vocab, float scale, float *__restrict__ d_table,
+                                                        float *__restrict__ part, int64_t sums, int rows_each)
+{
+    extern __shared__ int2 lds[];   // a chunk's places, those before and behind it at its ends
+    const int64_t group = workgroup();
+    if (group >= sums) {
+        const int64_t row0 = ((group - sums) * gridDim.y + blockIdx.y) * rows_each;
+        if (ADD || row0 >= vocab) return;
+        const int rows = vocab - row0 < rows_each ? (int)(vocab - row0) : rows_each;
+        int *const named = reinterpret_cast<int *>(lds);
+        if ((int)threadIdx.x < rows) {
+            const int row = (int)row0 + threadIdx.x;
+            int64_t lo = 0, hi = n;
+            while (lo < hi) {
+                const int64_t half = (lo + hi) >> 1;
+                if (sorted[half].x < row)
+                    lo = half + 1;
+                else
+                    hi = half;
+            }
+            named[threadIdx.x] = lo < n && sorted[lo].x == row;
+        }
+        __syncthreads();
+        // 16 bytes a thread side by side, whole rows one behind the other
+        const int across = lanes < kThreads / 2 ? 2 * lanes : kThreads, per = kThreads / across;
+        for (int r = threadIdx.x / across; r < rows; r += per) {
+            if (named[r]) continue;
+            float *const to = d_table + (row0 + r) * hidden;
+            for (int k = threadIdx.x % across * 4; k < hidden; k += 4 * across) {
+                if (k + 4 <= hidden) {
+                    typedef uint32_t Four __attribute__((ext_vector_type(4)));
+                    const Four none = {};
+                    __builtin_memcpy(to + k, &none, sizeof(none));
+                } else {
+                    for (int j = k; j < hidden; ++j) to[j] = 0.0f;
+                }
+            }
+        }
+        return;
+    }
+    const int mine = threadIdx.x / lanes;
+    const int64_t which = group * (kThreads / lanes) + mine, lo = which * chunk;
+    int2 *const at = lds + mine * (chunk + 2) + 1;   // at[-1] .. at[chunk]
+    for (int i = (int)(threadIdx.x % lanes) - 1; i <= chunk; i += lanes) {
+        const int64_t p = lo + i;
+        at[i] = p >= 0 && p < n ? sorted[p] : make_int2(p < 0 ? -1 : vocab, 0);
+    }
+    __syncthreads();
+    const Columns c(hidden, blockIdx.y * lanes + threadIdx.x % lanes);
+    if (lo >= n || c.skip >= 8) return;
+    float sum[8] = {};
+    for (int i0 = 0; i0 < chunk && at[i0].x != vocab; i0 += kRowsAhead) {
+        Words<T> w[kRowsAhead];
+        Words<float> old[ADD ? kRowsAhead : 1];
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u) w[u] = load_words(d_out + at[i0 + u].y * stride + c.first);
+        if constexpr (ADD)
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; ++u) {   // where no row ends: one that is in the cache
+                const int token = at[i0 + u].x;
+                const int row = token != vocab && at[i0 + u + 1].x != token ? token : at[i0].x;
+                old[u] = load_words(d_table + (int64_t)row * hidden + c.first);
+            }
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u) {
+            const int i = i0 + u, token = at[i].x;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += element<T>(w[u], j);
+            const bool goes_on = at[i + 1].x == token;
+            if (token == vocab || (goes_on && i + 1 < chunk)) continue;
+            const bool began = at[-1].x == token;
+            if (began || goes_on) {
+                put(part + (which * 2 + (began ? 0 : 1)) * hidden, c, sum);
+            } else {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = sum[j] * scale;
+                    if constexpr (ADD) v[j] += element<float>(old[u], j);
+                }
+                put(d_table + (int64_t)token * hidden, c, v);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+        }
     }
 }
 
-// The token that begins in chunk `workgroup` and goes on: its sums there and in the chunks that follow.
-template <int N>
-__global__ __launch_bounds__(kThreads) void k_embed_join(int64_t hidden, const int2 *__restrict__ sorted, int n,
-                                                         int chunk, int vocab, float scale, bool add,
-                                                         const float *__restrict__ part, float *__restrict__ d_table)
+// The token that begins in chunk `workgroup` and goes on: its sums there and in the chunks that follow, a run of them for
+// each quarter of the workgroup, then the quarters in their order.
+constexpr int kJoinThreads = 1024, kQuarters = kJoinThreads / kThreads;
+__global__ __launch_bounds__(kJoinThreads) void k_embed_join(int hidden, const int2 *__restrict__ sorted, int64_t n,
+                                                             int chunk, int vocab, float scale, bool add,
+                                                             const float *__restrict__ part, float *__restrict__ d_table)
 {
-    const int64_t h = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * N;
-    const int lo = blockIdx.x * chunk, hi = lo + chunk;
-    if (h >= hidden || hi >= n) return;
+    constexpr int kAhead = 8;
+    __shared__ float sh[kQuarters - 1][8][kThreads];
+    const int64_t which = workgroup(), lo = which * chunk, hi = lo + chunk;
+    if (hi >= n) return;
     const int token = sorted[hi - 1].x;
     if (token == vocab || sorted[hi].x != token || (lo > 0 && sorted[lo - 1].x == token)) return;
-    float sum[N];
-    const float *from = part + ((int64_t)blockIdx.x * 2 + 1) * hidden + h;
-#pragma unroll
-    for (int c = 0; c < N; ++c) sum[c] = from[c];
-    for (int i = hi; i < n && sorted[i].x == token; i += chunk) {
-        from = part + (int64_t)(i / chunk) * 2 * hidden + h;
-#pragma unroll
-        for (int c = 0; c < N; ++c) sum[c] += from[c];
+    int64_t chunks = 0;   // behind this one that begin with the token
+    for (int64_t a = 0, b = (n - hi + chunk - 1) / chunk; a < b;) {
+        const int64_t half = (a + b) >> 1;
+        if (sorted[hi + half * chunk].x == token)
+            a = half + 1;
+        else
+            b = half;
+        chunks = a;
     }
-    put<N>(d_table + token * hidden + h, sum, scale, add);
+    const int thread = threadIdx.x % kThreads, quarter = threadIdx.x / kThreads;
+    const Columns c(hidden, blockIdx.y * kThreads + thread);
+    const bool has = c.skip < 8;
+    // sum 0 is this chunk's, sum i of the chunk i behind it
+    const int64_t each = (chunks + kQuarters) / kQuarters, first = min(quarter * each, chunks + 1);
+    const int64_t last = min(first + each, chunks + 1);
+    const float *const from = part + which * 2 * hidden + c.first;
+    float sum[8] = {};
+    for (int64_t i = first; has && i < last; i += kAhead) {
+        Words<float> x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t at = min(i + u, last - 1);
+            x[u] = load_words(from + (at * 2 + (at == 0 ? 1 : 0)) * hidden);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u < last) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += element<float>(x[u], j);
+            }
+    }
+    if (quarter > 0)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sh[quarter - 1][j][thread] = sum[j];
+    __syncthreads();
+    if (quarter > 0 || !has) return;
+#pragma unroll
+    for (int q = 1; q < kQuarters; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += sh[q - 1][j][thread];
+    float *const row = d_table + (int64_t)token * hidden;
+    Words<float> old = {};
+    if (add) old = load_words(row + c.first);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = element<float>(old, j) + sum[j] * scale;
+    put(row, c, sum);
 }
 
-int chunk_of(int64_t tokens) { return tokens < 8192 ? 8 : 32; }
-int64_t chunks_of(int64_t tokens) { return ceil_div(tokens < kSegment ? tokens : kSegment, chunk_of(tokens)); }
+// Rows of less than 8 columns: a thread a row of the table, its places found by a search.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_embed_narrow(const T *__restrict__ d_out, int64_t stride, int hidden,
+                                                           const int2 *__restrict__ sorted, int64_t n, int vocab,
+                                                           float scale, bool add, float *__restrict__ d_table)
+{
+    const int64_t row = workgroup() * kThreads + threadIdx.x;
+    if (row >= vocab) return;
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t half = (lo + hi) >> 1;
+        if (sorted[half].x < row)
+            lo = half + 1;
+        else
+            hi = half;
+    }
+    float sum[8] = {};
+    bool any = false;
+    for (; lo < n && sorted[lo].x == row; ++lo, any = true) {
+        const T *const from = d_out + sorted[lo].y * stride;
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < hidden) sum[j] += to_f32(from[j]);
+    }
+    if (add && !any) return;
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+        if (j < hidden) d_table[row * hidden + j] = (add ? d_table[row * hidden + j] : 0.0f) + sum[j] * scale;
+}
+
+// Places of a chunk.  us by 32, 64, 128: 32,768 places: 131,072 x 4,096, tokens as words fall 535, 516, 547, all of one token 641,
+// 562, 548; 1,000 x 7,168 177, 160, 155 and 284, 194, 163.  Few places need many chunks.
+int chunk_of(int64_t tokens) { return tokens < 8192 ? 8 : tokens < 65536 ? 64 : kChunkMost; }
 
 template <typename F>
 hipError_t by_type(int type, F f)
@@ -214,19 +413,29 @@ hipError_t by_type(int type, F f)
 
 }  // namespace
 
-int64_t embed_ws_bytes(int64_t tokens, int64_t hidden) { return ceil_div(tokens, 2) * 16 + chunks_of(tokens) * 2 * hidden * 4; }
+// sorted places twice, the sums of tokens that go on beyond a chunk
+int64_t embed_ws_bytes(int64_t tokens, int64_t hidden)
+{
+    const int64_t places = ceil_div(tokens, 2) * 16;
+    return (tokens > kSegment ? 2 : 1) * places + ceil_div(tokens, chunk_of(tokens)) * 2 * hidden * 4;
+}
 
 hipError_t launch_embed(const void *token, bool wide, int64_t tokens, const void *table, int type, int64_t stride,
                         int64_t vocab, int64_t hidden, float scale, void *out, hipStream_t s)
 {
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        const int64_t bytes = sizeof(T) * 8;
-        const bool vec = hidden % 8 == 0 && stride % 8 == 0 && aligned(table, bytes) && aligned(out, bytes);
-        auto *kernel = wide ? (vec ? k_embed<T, int64_t, true> : k_embed<T, int64_t, false>)
-                            : (vec ? k_embed<T, int32_t, true> : k_embed<T, int32_t, false>);
-        hipLaunchKernelGGL(kernel, many(tokens, (unsigned)ceil_div(hidden, kThreads * (vec ? 8 : 1))), dim3(kThreads), 0,
-                           s, token, tokens, static_cast<const T *>(table), stride, vocab, hidden, scale,
+        const int lanes = hidden < 8 ? 1 : lanes_of(hidden);
+        auto kernel = [&](auto i) {
+            using I = decltype(i);
+            return lanes == 256   ? k_embed<T, I, 256>
+                   : lanes == 128 ? k_embed<T, I, 128>
+                   : lanes == 64  ? k_embed<T, I, 64>
+                                  : k_embed<T, I, 0>;
+        };
+        hipLaunchKernelGGL((wide ? kernel(int64_t()) : kernel(int32_t())),
+                           many(ceil_div(tokens, kThreads / lanes), (unsigned)ceil_div(hidden, lanes * 8)), dim3(kThreads), 0,
+                           s, token, tokens, static_cast<const T *>(table), stride, vocab, (int)hidden, lanes, scale,
                            static_cast<T *>(out));
         return hipGetLastError();
     });
@@ -236,27 +445,42 @@ hipError_t launch_embed_backward(const void *d_out, int type, int64_t stride, in
                                  const void *token, bool wide, int64_t vocab, float scale, bool add, float *d_table,
                                  void *ws, hipStream_t s)
 {
-    if (!add)
-        hipLaunchKernelGGL(k_zero, many(ceil_div(vocab * hidden, 4 * kThreads)), dim3(kThreads), 0, s, d_table,
-                           vocab * hidden);
-    if (tokens == 0) return hipGetLastError();
-    int2 *sorted = static_cast<int2 *>(ws);
-    float *part = reinterpret_cast<float *>(sorted + ceil_div(tokens, 2) * 2);
+    if (tokens == 0 && add) return hipSuccess;
+    const int64_t places = ceil_div(tokens, 2) * 2;
+    int2 *sorted = static_cast<int2 *>(ws), *other = sorted + places;
+    float *part = reinterpret_cast<float *>(tokens > kSegment ? other + places : other);
     int bits = 1;
     while (vocab >> bits) ++bits;
-    hipLaunchKernelGGL((wide ? k_sort<int64_t> : k_sort<int32_t>), dim3((unsigned)ceil_div(tokens, kSegment)),
-                       dim3(kSortThreads), 0, s, token, tokens, vocab, bits, sorted);
-    const int chunk = chunk_of(tokens);
+    if (tokens > 0)
+        hipLaunchKernelGGL((wide ? k_sort<int64_t> : k_sort<int32_t>), dim3((unsigned)ceil_div(tokens, kSegment)),
+                           dim3(kSortThreads), 0, s, token, tokens, vocab, bits, sorted);
+    for (int64_t run = kSegment; run < tokens; run *= kWays) {
+        hipLaunchKernelGGL(k_merge, many(ceil_div(tokens, kThreads)), dim3(kThreads), 0, s, sorted, other, (int)tokens,
+                           (int)run);
+        int2 *const t = sorted;
+        sorted = other, other = t;
+    }
+    const int chunk = chunk_of(tokens), lanes = lanes_of(hidden);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        for (int64_t first = 0; first < tokens; first += kSegment) {
-            const int n = (int)(tokens - first < kSegment ? tokens - first : kSegment);
-            const dim3 grid((unsigned)ceil_div(n, chunk), (unsigned)ceil_div(hidden, kThreads));
-            hipLaunchKernelGGL((k_embed_sum<T, 1>), grid, dim3(kThreads), 0, s, static_cast<const T *>(d_out), stride,
-                               hidden, sorted + first, n, chunk, (int)vocab, scale, add || first > 0, d_table, part);
-            hipLaunchKernelGGL((k_embed_join<1>), grid, dim3(kThreads), 0, s, hidden, sorted + first, n, chunk,
-                               (int)vocab, scale, add || first > 0, part, d_table);
+        const T *d = static_cast<const T *>(d_out);
+        if (hidden < 8) {
+            hipLaunchKernelGGL(k_embed_narrow<T>, many(ceil_div(vocab, kThreads)), dim3(kThreads), 0, s, d, stride,
+                               (int)hidden, sorted, tokens, (int)vocab, scale, add, d_table);
+            return hipGetLastError();
         }
+        const int64_t chunks = ceil_div(tokens, chunk), sums = ceil_div(chunks, kThreads / lanes);
+        const unsigned columns = (unsigned)ceil_div(hidden, lanes * 8);
+        // about 256 KB to clear a workgroup
+        const int64_t fit = ceil_div(256 << 10, hidden * 4), rows_each = fit < kThreads ? fit : kThreads;
+        const int64_t clears = add ? 0 : ceil_div(vocab, rows_each * columns);
+        const size_t lds = sizeof(int2) * (kThreads / lanes) * (chunk + 2);
+        hipLaunchKernelGGL((add ? k_embed_sum<T, true> : k_embed_sum<T, false>), many(sums + clears, columns),
+                           dim3(kThreads), lds > kThreads * 4 ? lds : kThreads * 4, s, d, stride, (int)hidden, sorted,
+                           tokens, chunk, lanes, (int)vocab, scale, d_table, part, sums, (int)rows_each);
+        if (chunks > 1)
+            hipLaunchKernelGGL(k_embed_join, many(chunks - 1, (unsigned)ceil_div(hidden, 8 * kThreads)),
+                               dim3(kJoinThreads), 0, s, (int)hidden, sorted, tokens, chunk, (int)vocab, scale, add, part, d_table);
         return hipGetLastError();
     });
 }
