@@ -86,22 +86,22 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const void *__restrict__ 
                                                        int bits, int2 *__restrict__ sorted)
 {
     __shared__ int key[kSegment];
-    __shared__ uint16_t order[2][kSegment], count[kSortWaves][kBins];
-    __shared__ int sh[kSortWaves];
+    __shared__ uint16_t order[2][kSegment];
+    __shared__ __attribute__((aligned(16))) uint16_t count[kSortWaves][kBins];
+    __shared__ int sh[kBins / 64];
+    static_assert(sizeof(count) == kSortThreads * 16, "a thread clears 16 bytes");
     const int64_t first = (int64_t)blockIdx.x * kSegment;
     const int n = tokens - first < kSegment ? (int)(tokens - first) : kSegment;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int i = threadIdx.x; i < n; i += kSortThreads) {
         const int64_t v = token_at<I>(token, first + i);
         key[i] = (uint64_t)v < (uint64_t)vocab ? (int)v : (int)vocab;
-        order[0][i] = (uint16_t)i;
     }
     const int run = (n + kSortThreads - 1) / kSortThreads * 64;   // a wave's
     const int lo = wave * run, hi = min(lo + run, n);
     int from = 0;
     for (int shift = 0; shift < bits; shift += kDigit, from ^= 1) {
-        const int digits = min(kDigit, bits - shift);
-        for (int i = threadIdx.x; i < kSortWaves * kBins; i += kSortThreads) (&count[0][0])[i] = 0;
+        reinterpret_cast<uint4 *>(count)[threadIdx.x] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         int held[kSteps], rank[kSteps];   // place and digit, rank among the wave's of its digit
 #pragma unroll
@@ -109,12 +109,14 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const void *__restrict__ 
             const int i = lo + s * 64 + lane;
             if (lo + s * 64 >= hi) break;
             const bool in = i < hi;
-            const int place = in ? order[from][i] : 0;
-            const int digit = in ? key[place] >> shift & ((1 << digits) - 1) : 0;
+            const int place = !in ? 0 : shift == 0 ? i : order[from][i];
+            const int digit = in ? key[place] >> shift & (kBins - 1) : 0;
             uint64_t same = __ballot(in);
-            for (int b = 0; b < digits; ++b) {
-                const uint64_t on = __ballot(digit >> b & 1);
-                same &= digit >> b & 1 ? on : ~on;
+#pragma unroll
+            for (int b = 0; b < kDigit; ++b) {
+                const bool one = digit >> b & 1;
+                const uint64_t on = __ballot(one);
+                same &= one ? on : ~on;
             }
             const uint64_t below = same & ((1ull << lane) - 1);
             held[s] = place | digit << 16;
@@ -128,31 +130,44 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const void *__restrict__ 
         }
         __syncthreads();
         // where each wave's places of a digit begin: those of lower digits, then of the waves before
-        int total = 0, inc;
-        if (threadIdx.x < kBins)
+        if (threadIdx.x < kBins) {
+            int own[kSortWaves], total = 0;
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) own[w] = count[w][threadIdx.x];
+#pragma unroll
             for (int w = 0; w < kSortWaves; ++w) {
-                const int c = count[w][threadIdx.x];
-                count[w][threadIdx.x] = (uint16_t)total;
+                const int c = own[w];
+                own[w] = total;
                 total += c;
             }
-        inc = total;
+            int inc = total;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(inc, d, 64);
-            if (lane >= d) inc += o;
-        }
-        if (lane == 63) sh[wave] = inc;
-        __syncthreads();
-        if (threadIdx.x < kBins) {
-            int before = inc - total;
-            for (int w = 0; w < wave; ++w) before += sh[w];
-            for (int w = 0; w < kSortWaves; ++w) count[w][threadIdx.x] += (uint16_t)before;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(inc, d, 64);
+                if (lane >= d) inc += o;
+            }
+            if (lane == 63) sh[wave] = inc;
+            const int before = inc - total;
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) count[w][threadIdx.x] = (uint16_t)(own[w] + before);
         }
         __syncthreads();
+        // the digits' totals by 64: each thread adds what is before its own digits
+        int base[kBins / 64], sum = 0;
+#pragma unroll
+        for (int g = 0; g < kBins / 64; ++g) {
+            base[g] = sum;
+            sum += sh[g];
+        }
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int i = lo + s * 64 + lane;
-            if (i < hi) order[from ^ 1][count[wave][held[s] >> 16] + rank[s]] = (uint16_t)(held[s] & 0xffff);
+            if (i >= hi) continue;
+            const int digit = held[s] >> 16;
+            int before = 0;
+#pragma unroll
+            for (int g = 1; g < kBins / 64; ++g) before = digit >> 6 == g ? base[g] : before;
+            order[from ^ 1][before + count[wave][digit] + rank[s]] = (uint16_t)(held[s] & 0xffff);
         }
         __syncthreads();
     }

@@ -197,6 +197,13 @@ __device__ inline float dpp(float x)
     return __builtin_bit_cast(float, dpp<CTRL>(__builtin_bit_cast(int, x)));
 }
 
+template <int CTRL>
+__device__ inline double dpp(double x)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)dpp<CTRL>((int)(b >> 32)) << 32 | (uint32_t)dpp<CTRL>((int)b));
+}
+
 // Over the 16 lanes of a row, the result in each of them: rotations of the row by 8, 4, 2 and 1.
 template <typename V, typename F>
 __device__ inline V row_reduce(V v, F f)
@@ -214,8 +221,27 @@ __device__ inline V wave_reduce(V v, F f)
     v = f(v, __shfl_xor(v, 16, 64));
     return f(v, __shfl_xor(v, 32, 64));
 }
+// The same by way of scalars, where a wave waits for it: two trips through LDS' crossbar less.
+template <typename V>
+__device__ inline V lane_value(V v, int lane)
+{
+    if constexpr (sizeof(V) == 8) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 |
+                                         (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
+    } else {
+        return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    }
+}
+template <typename V, typename F>
+__device__ inline V wave_value(V v, F f)
+{
+    v = row_reduce(v, f);
+    return f(f(lane_value(v, 0), lane_value(v, 16)), f(lane_value(v, 32), lane_value(v, 48)));
+}
 struct Max {
     __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+    __device__ double operator()(double a, double b) const { return fmax(a, b); }
     __device__ int operator()(int a, int b) const { return a > b ? a : b; }
 };
 struct Min {
@@ -223,6 +249,7 @@ struct Min {
 };
 struct Sum {
     __device__ float operator()(float a, float b) const { return a + b; }
+    __device__ double operator()(double a, double b) const { return a + b; }
     __device__ int operator()(int a, int b) const { return a + b; }
 };
 #endif

@@ -2,188 +2,417 @@
 // best groups of experts, the best experts of those; weights from the scores without the bias.
 //
 // The choice is that of the exact scores: with a bias no order of the logits tells it, and two sums s + bias can be
-// nearer to each other than fp32 resolves.  So they are computed in 64 bits.
+// nearer to each other than fp32 resolves.  So a token is chosen for in fp32 first, by 16 lanes as in route.hip, and each
+// pair of neighbours in the order that decides something is looked at: the chosen experts, the first that is not, the last
+// group that stays and the first that does not.  Where one is nearer than the error of the two (about one token in a
+// thousand), the wave computes that token's scores again in 64 bits.
 #include "router.h"
 
 namespace hapmoe {
 namespace {
 
-constexpr int kChooseThreads = 512;
-
-__device__ inline double wave_max(double v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = fmax(v, __shfl_xor(v, d, 64));
-    return v;
-}
-__device__ inline double wave_sum(double v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-    return v;
-}
-__device__ inline float wave_max(float v) { return wave_reduce(v, Max()); }
-
-struct Choice {
-    float x;     // the logit
-    int expert;  // -1: none
-};
-
-// One token by a wave, its choice j in lane j; lane's experts are lane * N .. lane * N + N.  total: of exp(x - top).
+// One token by a wave in 64 bits, expert i * 64 + lane in a lane's i-th place: its choices to chosen[top_k].  c: [experts]
+// and [64] of the wave's LDS.  Of a softmax the largest logit and the sum of exp(x - top) too.
 template <typename T, int N>
-__device__ inline Choice choose_exactly(const T *__restrict__ row, const float *__restrict__ bias, int experts,
-                                        int top_k, bool sigmoid, int groups, int top_groups, int group_best, bool keep,
-                                        float &top, float &total)
+__device__ inline void choose_exactly(const BalancedRoute &q, const T *__restrict__ row, bool keep, double *c, int *chosen,
+                                      float &top, float &total)
 {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, experts = q.experts, each = experts / q.groups;
     float x[N];
-    double c[N];
+    double v[N], sum = 0.0;
     top = -INFINITY;
 #pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = to_f32(row[min(i * 64 + lane, experts - 1)]);
+#pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int e = lane * N + i;
-        x[i] = keep && e < experts ? to_f32(row[e]) : -INFINITY;
-        x[i] = x[i] > -INFINITY ? x[i] : -INFINITY;
+        x[i] = keep && i * 64 + lane < experts && x[i] > -INFINITY ? x[i] : -INFINITY;
         top = fmaxf(top, x[i]);
     }
-    top = wave_max(top);
-    double sum = 0.0;
+    if (!q.sigmoid) top = wave_value(top, Max());
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (sigmoid)
-            c[i] = 1.0 / (1.0 + exp(-(double)x[i]));
-        else
-            sum += c[i] = x[i] == top ? 1.0 : exp((double)x[i] - (double)top);   // top closed: not read below
+        v[i] = exp(q.sigmoid ? -(double)x[i] : x[i] == top ? 0.0 : (double)x[i] - (double)top);
+        if (i * 64 + lane < experts) sum += v[i];
     }
-    if (!sigmoid) {
-        sum = wave_sum(sum);
-        total = (float)sum;
-    }
+    if (!q.sigmoid) sum = wave_value(sum, Sum());
+    total = (float)sum;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (!sigmoid) c[i] /= sum;
-        const int e = lane * N + i;
-        if (bias && e < experts) c[i] += (double)bias[e];
+        v[i] = (q.sigmoid ? 1.0 : v[i]) / (q.sigmoid ? 1.0 + v[i] : sum);
+        if (q.bias) v[i] += (double)q.bias[min(i * 64 + lane, experts - 1)];
         // closed to the choice: closed by its logit, or by a bias of -inf or NaN
-        c[i] = x[i] > -INFINITY && c[i] > -INFINITY ? c[i] : -INFINITY;
+        v[i] = x[i] > -INFINITY && v[i] > -INFINITY ? v[i] : -INFINITY;
     }
-    if (top_groups < groups) {
-        const int each = experts / groups;
-        double mine = -INFINITY;   // of group `lane`
-        for (int g = 0; g < groups; ++g) {
-            double first = -INFINITY;
-            int at = -1;
+    if (q.top_groups < q.groups) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int e = lane * N + i;
-                if (e >= g * each && e < g * each + each && c[i] > first) first = c[i], at = i;
+        for (int i = 0; i < N; ++i)
+            if (i * 64 + lane < experts) c[i * 64 + lane] = v[i];
+        wave_order();
+        double first = -INFINITY, next = -INFINITY;   // of group `lane`
+        if (lane < q.groups)
+#pragma unroll 4
+            for (int i = 0; i < each; ++i) {
+                const double s = c[lane * each + i];
+                next = fmax(next, fmin(first, s));
+                first = fmax(first, s);
             }
-            const double best = wave_max(first);
-            double score = best;
-            if (group_best > 1) {
-                const uint64_t who = __ballot(first == best && at >= 0);
-                const bool out = who != 0 && lane == __ffsll((unsigned long long)who) - 1;
-                double next = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int e = lane * N + i;
-                    if (e >= g * each && e < g * each + each && !(out && i == at)) next = fmax(next, c[i]);
-                }
-                next = wave_max(next);
-                if (next > -INFINITY) score += next;
-            }
-            if (lane == g) mine = score;
-        }
+        if (q.group_best > 1 && next > -INFINITY) first += next;
+        wave_order();
+        c[lane] = first;   // the groups' scores in the experts' place, which is at least that long
+        wave_order();
         int before = 0;   // groups that go before this lane's
-        for (int g = 0; g < groups; ++g) {
-            const double other = __shfl(mine, g, 64);
-            before += other > mine || (other == mine && g < lane);
-        }
-        const uint64_t taken = __ballot(lane < groups && before < top_groups);
+#pragma unroll 4
+        for (int g = 0; g < q.groups; ++g) before += c[g] > first || (c[g] == first && g < lane);
+        const uint64_t taken = __ballot(lane < q.groups && before < q.top_groups);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int e = lane * N + i;
-            if (e >= experts || !(taken >> (e / each) & 1)) c[i] = -INFINITY;
-        }
+        for (int i = 0; i < N; ++i)
+            if (i * 64 + lane >= experts || !(taken >> ((i * 64 + lane) / each) & 1)) v[i] = -INFINITY;
     }
-    if (!bias) {   // the scores' order is that of the logits
+    if (!q.bias) {   // the scores' order is that of the logits
 #pragma unroll
-        for (int i = 0; i < N; ++i) c[i] = c[i] > -INFINITY ? (double)x[i] : -INFINITY;
+        for (int i = 0; i < N; ++i) v[i] = v[i] > -INFINITY ? (double)x[i] : -INFINITY;
     }
-    Choice won = {-INFINITY, -1};
-    for (int j = 0; j < top_k; ++j) {
-        double own = c[0];
-        float own_x = x[0];
-        int at = 0;
+    for (int j = 0; j < q.top_k; ++j) {
+        double own = v[0];
+        int at = lane;
 #pragma unroll
         for (int i = 1; i < N; ++i) {
-            const bool more = c[i] > own;
-            own = more ? c[i] : own;
-            own_x = more ? x[i] : own_x;
-            at = more ? i : at;
+            at = v[i] > own ? i * 64 + lane : at;
+            own = fmax(own, v[i]);
         }
-        const double best = wave_max(own);
-        if (best == -INFINITY) break;
-        const int from = __ffsll((unsigned long long)__ballot(own == best)) - 1;
-        const int which = __shfl(at, from, 64);
-        const float value = __shfl(own_x, from, 64);
-        if (lane == j) won = {value, from * N + which};
-        if (lane == from) {
+        const double best = wave_value(own, Max());
+        const int won = best > -INFINITY ? wave_value(own == best ? at : INT32_MAX, Min()) : -1;
 #pragma unroll
-            for (int i = 0; i < N; ++i) c[i] = i == which ? -INFINITY : c[i];
-        }
+        for (int i = 0; i < N; ++i) v[i] = won == i * 64 + lane ? -INFINITY : v[i];
+        if (lane == 0) chosen[j] = won;
     }
-    return won;
 }
 
-template <typename T, int N, bool ALONE>
-__global__ __launch_bounds__(kChooseThreads) void k_choose_balanced(
-    const T *__restrict__ logits, int64_t stride, int64_t tokens, int experts, int top_k,
-    const float *__restrict__ bias, int sigmoid, int groups, int top_groups, int group_best,
-    const uint8_t *__restrict__ keep, int renormalize, float scale, int group, int bits, float *__restrict__ weight,
-    int32_t *__restrict__ expert, int32_t *__restrict__ place, int32_t *__restrict__ hist, int32_t *__restrict__ count,
-    int32_t *__restrict__ offset, int32_t *__restrict__ slot)
+// Groups of whole lanes, 1, 2, 4, 8 or 16 of them; 0: any others.
+__host__ __device__ inline int lanes_a_group(int each, int per)
 {
-    constexpr int kWaves = kChooseThreads / 64;
-    extern __shared__ __attribute__((aligned(16))) int lds[];
-    const int64_t first = workgroup() * group;
-    if (first >= tokens && first > 0) return;
-    const int here = tokens - first < group ? (int)(tokens - first) : group;
-    int *const chosen = lds;
-    int *const sums = lds + ((here * top_k + 3) & ~3);
-    __shared__ int sh[kWaves];
-    const int lane = threadIdx.x & 63;
-    for (int e = threadIdx.x; e < kWaves * experts; e += kChooseThreads) sums[e] = 0;
-    for (int t0 = threadIdx.x >> 6; t0 < here; t0 += kWaves) {
-        const int64_t t = first + t0;
-        float top, total = 1.0f;
-        const Choice c = choose_exactly<T, N>(logits + t * stride, bias, experts, top_k, sigmoid, groups, top_groups,
-                                              group_best, !keep || keep[t], top, total);
-        const bool has = c.expert >= 0;
-        float share;
-        if (!renormalize) {
-            share = !has ? 0.0f : sigmoid ? sigmoid_of(c.x) : exp_from(c.x, top) / total;
-        } else {
-            // the scores over that of the largest logit chosen, a factor that they share left out: none underflows to 0 / 0
-            const float most = wave_max(c.x);
-            if (sigmoid) {
-                share = exp_from(fminf(c.x, 0.0f), fminf(most, 0.0f)) / (1.0f + exp_from(-fabsf(c.x), 0.0f));
-            } else {
-                share = exp_from(c.x, most);
-            }
-            share = has ? share : 0.0f;
-            const float sum = wave_reduce(share, Sum());
-            share = has ? share / sum : 0.0f;
+    const int m = each / per;
+    return each % per == 0 && (m & (m - 1)) == 0 ? m : 0;
+}
+
+struct Top2 {
+    int a, b;   // keys, the largest and the next
+    __device__ void take(int k)
+    {
+        b = Max()(b, Min()(a, k));
+        a = Max()(a, k);
+    }
+    __device__ void join(int oa, int ob)
+    {
+        b = Max()(Min()(a, oa), Max()(b, ob));
+        a = Max()(a, oa);
+    }
+    // The other lanes of a group of m (a power of two), neighbours in a row of 16.
+    __device__ void over_lanes(int m)
+    {
+        if (m >= 2) join(dpp<0xb1>(a), dpp<0xb1>(b));     // lanes 1 0 3 2
+        if (m >= 4) join(dpp<0x4e>(a), dpp<0x4e>(b));     // lanes 2 3 0 1
+        if (m >= 8) join(dpp<0x141>(a), dpp<0x141>(b));   // 8 lanes mirrored: the other four's
+        if (m >= 16) join(dpp<0x140>(a), dpp<0x140>(b));  // 16 lanes mirrored
+    }
+    // The group's score, and its summands' size for the error.
+    __device__ int score(int group_best, float &size) const
+    {
+        if (a == kClosed) return kClosed;
+        const float x = logit_of(a), y = group_best > 1 && b != kClosed ? logit_of(b) : 0.0f;
+        size = fmaxf(size, fabsf(x) + fabsf(y));
+        return key_of(x + y);
+    }
+};
+
+// Of a row of 16 lanes the groups that stay.  largest(): a lane's best score; find(most): the lowest group that a lane has
+// it for; close(g).  near: whether the last of them and the first that goes are within `error` of each other.
+template <typename L, typename F, typename C>
+__device__ inline uint64_t best_groups(int top_groups, float error, bool &near, L largest, F find, C close)
+{
+    uint64_t taken = 0;
+    float last = 0.0f;
+    for (int j = 0;; ++j) {
+        const int most = row_reduce(largest(), Max());
+        if (most == kClosed) break;
+        const float value = logit_of(most);
+        if (j == top_groups) {
+            near = !(last - value > error);
+            break;
         }
-        if (lane < top_k) {
-            weight[t * top_k + lane] = share * scale;
-            expert[t * top_k + lane] = c.expert;
-            chosen[t0 * top_k + lane] = c.expert;
+        const int g = row_reduce(find(most), Min());
+        taken |= 1ull << g;
+        close(g);
+        last = value;
+    }
+    return taken;
+}
+
+// Weights from the logit z of a lane's choice or choices (-inf: none), N a lane; reduce: over the token's lanes.
+template <bool SIGMOID, int N, typename R>
+__device__ inline void shares(const float *z, float *share, bool renormalize, float top, float total, R reduce)
+{
+    if (!renormalize) {
+#pragma unroll
+        for (int h = 0; h < N; ++h) share[h] = SIGMOID ? sigmoid_of(z[h]) : exp_from(z[h], top) / total;
+    } else {
+        // the scores over that of the largest logit chosen, a factor that they share left out: none underflows to 0 / 0
+        float largest = z[0], sum = 0.0f;
+#pragma unroll
+        for (int h = 1; h < N; ++h) largest = fmaxf(largest, z[h]);
+        largest = reduce(largest, Max());
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            share[h] = SIGMOID ? exp_from(fminf(z[h], 0.0f), fminf(largest, 0.0f)) / (1.0f + exp_from(-fabsf(z[h]), 0.0f))
+                               : exp_from(z[h], largest);
+            share[h] = z[h] > -INFINITY ? share[h] : 0.0f;
+            sum += share[h];
+        }
+        sum = reduce(sum, Sum());
+#pragma unroll
+        for (int h = 0; h < N; ++h) share[h] /= sum;
+    }
+}
+
+constexpr int kAgain = -2;   // in place of a token's first choice: it is chosen for again
+
+// LDS: [here * top_k] choices, then the tokens' keys and, where groups are not whole lanes, their scores; when those are
+// done the counts of the order.
+template <typename T, int PER, bool VEC, bool ALONE, bool SIGMOID>
+__global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(BalancedRoute q, int group, int bits)
+{
+    constexpr int kChoose = choose_threads(PER), kWaves = kChoose / 64;
+    constexpr float kUnit = 1.0f / (1 << 22), kLog2 = 1.44269504f;
+    extern __shared__ __attribute__((aligned(16))) int lds[];
+    __shared__ int sh[kWaves];
+    const int64_t first = workgroup() * group;
+    if (first >= q.tokens && first > 0) return;
+    const int here = q.tokens - first < group ? (int)(q.tokens - first) : group;
+    const int experts = q.experts, top_k = q.top_k, each = experts / q.groups;
+    int *const chosen = lds;
+    int *const sums = lds + ((here * top_k + 3) & ~3);   // whole vectors
+    const int lane = threadIdx.x & 15, wave_lane = threadIdx.x & 63;
+    int *const row = sums + (threadIdx.x >> 4) * key_row(PER);
+    const int m = lanes_a_group(each, PER);
+    const bool grouped = q.top_groups < q.groups, scored = q.bias || grouped || (!SIGMOID && !q.renormalize);
+    for (int base = (threadIdx.x >> 6) * 4; base < here; base += kChoose / 16) {   // the same in a wave
+        const int t0 = min(base + (wave_lane >> 4), here - 1);
+        const int64_t t = first + t0;
+        const T *const logits = static_cast<const T *>(q.logits) + t * q.stride;
+        const bool keep = !q.keep || q.keep[t];
+        float x[PER];
+        int v[PER];
+        load_logits<T, PER, VEC, true>(x, logits, lane, experts, keep);
+        float top = -INFINITY, total = 1.0f, error = 2 * kUnit;
+        if (scored) {
+            // A sigmoid by exp2 and rcp, a unit each: its error is below 2^-22, as |x| s (1 - s) < 1/4.  A share of the softmax:
+            // below (PER / 2 + 14) 2^-23 of the largest share, PER / 2 + 2 by the sum, 10 by exponents of up to the entropy's
+            // 11 bits.  Twice that for the difference of two.
+            if constexpr (SIGMOID) {
+#pragma unroll
+                for (int c = 0; c < PER; ++c)
+                    x[c] = x[c] > -INFINITY ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[c] * -kLog2)) : -INFINITY;
+            } else {
+                top = row_reduce(lane_largest<float, PER>(x), Max());
+                total = 0.0f;
+#pragma unroll
+                for (int c = 0; c < PER; ++c) {
+                    const float e = x[c] == top ? 1.0f : __builtin_amdgcn_exp2f((x[c] - top) * kLog2);
+                    total += e;
+                    x[c] = x[c] > -INFINITY ? e : -INFINITY;
+                }
+                total = row_reduce(total, Sum());   // of a closed token 16 * PER
+                const float size = __builtin_amdgcn_rcpf(total);
+                error = (PER / 2 + 14) * kUnit * size;
+#pragma unroll
+                for (int c = 0; c < PER; ++c) x[c] *= size;
+            }
+            if (q.bias) {
+                int at = lane * PER;
+                asm volatile("" : "+v"(at));   // loaded for every token: held they are as many registers as the keys
+#pragma unroll
+                for (int c = 0; c < PER; ++c) x[c] += q.bias[VEC ? at + c : min(at + c, experts - 1)];
+            }
+#pragma unroll
+            for (int c = 0; c < PER; ++c) v[c] = x[c] > -INFINITY ? key_of(x[c]) : kClosed;   // a NaN bias closes too
+        } else {
+#pragma unroll
+            for (int c = 0; c < PER; ++c) v[c] = key_of(x[c]);
+        }
+        bool again = false, near = false;   // in the choice of groups, of experts
+        if (grouped) {
+            float size = 0.0f;
+            if (m > 0) {
+                Top2 best = {v[0], kClosed};
+#pragma unroll
+                for (int c = 1; c < PER; ++c) best.take(v[c]);
+                best.over_lanes(m);
+                int key = best.score(q.group_best, size);
+                const int mine = lane / m;
+                size = row_reduce(size, Max());
+                const uint64_t taken = best_groups(
+                    q.top_groups, 2 * error + kUnit * size, again, [&] { return key; },
+                    [&](int most) { return key == most ? mine : INT32_MAX; }, [&](int g) { key = g == mine ? kClosed : key; });
+#pragma unroll
+                for (int c = 0; c < PER; ++c) v[c] = taken >> mine & 1 ? v[c] : kClosed;
+            } else {
+                int *const score = sums + kChoose / 16 * key_row(PER) + (threadIdx.x >> 4) * HAPMOE_MAX_GROUPS;
+                wave_order();
+#pragma unroll
+                for (int c = 0; c < PER; c += 4)
+                    *reinterpret_cast<int4 *>(row + lane * PER + c) = make_int4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+                wave_order();
+#pragma unroll 1
+                for (int g = lane; g < q.groups; g += 16) {
+                    Top2 best = {kClosed, kClosed};
+#pragma unroll 1
+                    for (int i = 0; i < each; ++i) best.take(row[g * each + i]);
+                    score[g] = best.score(q.group_best, size);
+                }
+                size = row_reduce(size, Max());
+                const uint64_t taken = best_groups(
+                    q.top_groups, 2 * error + kUnit * size, again,
+                    [&] {
+                        int own = kClosed;
+#pragma unroll 1
+                        for (int g = lane; g < q.groups; g += 16) own = Max()(own, score[g]);
+                        return own;
+                    },
+                    [&](int most) {
+                        int g = lane;
+#pragma unroll 1
+                        while (g < q.groups && score[g] != most) g += 16;
+                        return g < q.groups ? g : INT32_MAX;
+                    },
+                    [&](int g) {
+                        if (g % 16 == lane) score[g] = kClosed;
+                    });
+                int g = lane * PER / each;
+                asm volatile("" : "+v"(g));   // the groups of PER experts again for every token, not in registers
+                int in = lane * PER - g * each;
+#pragma unroll
+                for (int c = 0; c < PER; ++c) {
+                    v[c] = g < q.groups && taken >> g & 1 ? v[c] : kClosed;
+                    if (++in == each) in = 0, ++g;
+                }
+            }
+        }
+        if (!q.bias && scored) {   // the scores' order is that of the logits
+            load_logits<T, PER, VEC, true>(x, logits, lane, experts, keep);
+#pragma unroll
+            for (int c = 0; c < PER; ++c) v[c] = v[c] == kClosed ? kClosed : key_of(x[c]);
+        }
+        wave_order();   // the keys before are read
+#pragma unroll
+        for (int c = 0; c < PER; c += 4)
+            *reinterpret_cast<int4 *>(row + lane * PER + c) = make_int4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+        wave_order();
+        int own = lane_largest<int, PER>(v), most = row_reduce(own, Max());
+        int who[2] = {-1, -1};   // choices lane and lane + 16
+        int before = -1;         // the choice before, where this one is near to it
+        for (int j = 0; j <= top_k && most != kClosed && (j < top_k || before >= 0); ++j) {
+            const int from = first_of_row(own == most);
+            int best;
+            if constexpr (PER >= 16) {
+                int k[PER / 16], at = 0;
+#pragma unroll
+                for (int i = 0; i < PER / 16; ++i) k[i] = row[from * PER + 16 * i + lane];
+#pragma unroll
+                for (int i = PER / 16 - 1; i >= 0; --i) {
+                    const int l = first_of_row(k[i] == most);
+                    at = l < 16 ? 16 * i + l : at;
+                }
+                best = from * PER + at;
+#pragma unroll
+                for (int i = 0; i < PER / 16; ++i) k[i] = at == 16 * i + lane ? kClosed : k[i];
+                if (lane == 0) row[best] = kClosed;
+                wave_order();
+                const int left = row_reduce(lane_largest<int, PER / 16>(k), Max());
+                own = lane == from ? left : own;
+            } else {
+                const int k = lane < PER ? row[from * PER + lane] : kClosed;
+                const int at = first_of_row(k == most);
+                best = from * PER + at;
+                if (lane == 0) row[best] = kClosed;
+                wave_order();
+                const int left = row_reduce(lane == at ? kClosed : k, Max());
+                own = lane == from ? left : own;
+            }
+            // equal logits and biases have equal sums, however near; others may not be in this order
+            if (before >= 0)
+                near = near || to_f32(logits[before]) != to_f32(logits[best]) || q.bias[before] != q.bias[best];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) who[h] = lane + 16 * h == j ? best : who[h];
+            const float value = logit_of(most);
+            most = row_reduce(own, Max());
+            before = q.bias && most != kClosed && !(value - logit_of(most) > error + kUnit / 2 * fabsf(value)) ? best : -1;
+        }
+        // Of up to 15 choices and the first that is not, where it is near to the last, sigmoids in 64 bits are one a lane: they
+        // are put in order here.  All else that is near takes a wave; so does an expert that is near to the first not chosen.
+        again = again || before >= 0 || (near && (!SIGMOID || top_k > 15));
+        if (SIGMOID && __ballot(near && !again)) {
+            const int e = who[0];
+            double sum = -INFINITY;
+            if (e >= 0) sum = 1.0 / (1.0 + exp(-(double)to_f32(logits[e]))) + (double)(q.bias ? q.bias[e] : 0.0f);
+            int rank = 0, other_e = e;
+            double other = sum;
+#pragma unroll 1
+            for (int i = 1; i < 16; ++i) {
+                other = dpp<0x121>(other), other_e = dpp<0x121>(other_e);   // the next lane's of the row
+                rank += other > sum || (other == sum && other_e >= 0 && other_e < e);
+            }
+            wave_order();
+            if (near && !again && e >= 0) row[rank] = e;
+            wave_order();
+            if (near && !again && e >= 0) who[0] = row[lane];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) who[h] = lane + 16 * h < top_k ? who[h] : -1;
+        float z[2], share[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) z[h] = who[h] >= 0 ? to_f32(logits[who[h]]) : -INFINITY;
+        shares<SIGMOID, 2>(z, share, q.renormalize, top, total, [](float x, auto f) { return row_reduce(x, f); });
+        if (base + (wave_lane >> 4) < here) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = lane + 16 * h;
+                if (j < top_k) chosen[t0 * top_k + j] = again && j == 0 ? kAgain : who[h];
+                if (j < top_k && !again) {
+                    q.weight[t * top_k + j] = who[h] >= 0 ? share[h] * q.scale : 0.0f;
+                    q.expert[t * top_k + j] = who[h];
+                }
+            }
         }
     }
     __syncthreads();
-    order_rows<kChooseThreads, ALONE>(chosen, sums, sh, here, top_k, first, experts, bits, place, hist, count, offset,
-                                      slot);
+    // the tokens that are left, a wave for each in turn
+    int number = 0;
+    uint64_t left = __ballot(wave_lane < here && chosen[min(wave_lane, here - 1) * top_k] == kAgain);
+    __syncthreads();   // every wave has them before the first is replaced
+    for (; left; left &= left - 1) {
+        if (number++ % kWaves != (int)(threadIdx.x >> 6)) continue;
+        const int t0 = __ffsll((unsigned long long)left) - 1;
+        const int64_t t = first + t0;
+        const T *const logits = static_cast<const T *>(q.logits) + t * q.stride;
+        float top, total, z, share;
+        // the wave's four rows of keys are done with, and as long as twice the experts
+        choose_exactly<T, PER / 4>(q, logits, !q.keep || q.keep[t],
+                                   reinterpret_cast<double *>(sums + (threadIdx.x >> 6) * 4 * key_row(PER)),
+                                   chosen + t0 * top_k, top, total);
+        wave_order();
+        const int who = wave_lane < top_k ? chosen[t0 * top_k + wave_lane] : -1;
+        z = who >= 0 ? to_f32(logits[who]) : -INFINITY;
+        shares<SIGMOID, 1>(&z, &share, q.renormalize, top, total, [](float x, auto f) { return wave_reduce(x, f); });
+        if (wave_lane < top_k) {
+            q.weight[t * top_k + wave_lane] = who >= 0 ? share * q.scale : 0.0f;
+            q.expert[t * top_k + wave_lane] = who;
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
+    __syncthreads();
+    order_rows<kChoose, ALONE>(chosen, sums, sh, here, top_k, first, experts, bits, q.place, static_cast<int32_t *>(q.ws),
+                               q.count, q.offset, q.slot);
 }
 
 }  // namespace
@@ -196,23 +425,29 @@ hipError_t launch_route_balanced(const BalancedRoute &a, hipStream_t s)
     int bits = 1;
     while ((1 << bits) <= a.experts) ++bits;   // of the keys 0 .. experts
     const int rows_here = (int)(a.tokens < group ? a.tokens : group) * a.top_k;
-    const size_t lds = (((rows_here + 3) & ~3) + (kChooseThreads / 64 + (alone ? 1 : 0)) * a.experts) * sizeof(int);
-    int32_t *hist = static_cast<int32_t *>(a.ws);
     const hipError_t e = by_type(a.type, [&](auto t) {
         using T = decltype(t);
         return by_experts(a.experts, [&](auto per) {
-            constexpr int N = decltype(per)::value / 4;
-            hipLaunchKernelGGL((alone ? k_choose_balanced<T, N, true> : k_choose_balanced<T, N, false>),
-                               many(workgroups), dim3(kChooseThreads), lds, s, static_cast<const T *>(a.logits),
-                               a.stride, a.tokens, a.experts, a.top_k, a.bias, a.sigmoid ? 1 : 0, a.groups, a.top_groups,
-                               a.group_best, a.keep, a.renormalize ? 1 : 0, a.scale, group, bits, a.weight, a.expert,
-                               a.place, hist, a.count, a.offset, a.slot);
+            constexpr int PER = decltype(per)::value;
+            constexpr int kChoose = choose_threads(PER);
+            const bool vec = a.experts == 16 * PER && aligned(a.logits, 16) && a.stride * (int64_t)sizeof(T) % 16 == 0;
+            const int sums = (kChoose / 64 + (alone ? 1 : 0)) * a.experts, keys = kChoose / 16 * key_row(PER);
+            const bool any = a.top_groups < a.groups && lanes_a_group(a.experts / a.groups, PER) == 0;
+            const int scores = any ? kChoose / 16 * HAPMOE_MAX_GROUPS : 0;
+            const size_t lds = (((rows_here + 3) & ~3) + (keys + scores > sums ? keys + scores : sums)) * sizeof(int);
+            auto kernel = [&](auto sigmoid) {
+                constexpr bool S = decltype(sigmoid)::value;
+                return alone ? (vec ? k_choose_balanced<T, PER, true, true, S> : k_choose_balanced<T, PER, false, true, S>)
+                             : (vec ? k_choose_balanced<T, PER, true, false, S> : k_choose_balanced<T, PER, false, false, S>);
+            };
+            hipLaunchKernelGGL((a.sigmoid ? kernel(std::true_type()) : kernel(std::false_type())), many(workgroups),
+                               dim3(kChoose), lds, s, a, group, bits);
             return hipGetLastError();
         });
     });
     if (e != hipSuccess || alone) return e;
-    return launch_route_order(a.expert, hist, workgroups, a.tokens * a.top_k, a.experts, group * a.top_k, a.count,
-                              a.offset, a.place, a.slot, s);
+    return launch_route_order(a.expert, static_cast<int32_t *>(a.ws), workgroups, a.tokens * a.top_k, a.experts,
+                              group * a.top_k, a.count, a.offset, a.place, a.slot, s);
 }
 
 }  // namespace hapmoe
