@@ -10,6 +10,8 @@ what its operators take:
     python -m paper_2609_39350_amd.measure --config 2 --type 2
 
 prints the measurement and the plans before and after, both with the workload's router counts.
+``--scores sigmoid --groups 8 --top-groups 4`` measures a router whose choice is balanced, and ``--block``
+what stands around the layer too: embedding, norm, and dropout onto the residual.
 """
 from __future__ import annotations
 
@@ -25,23 +27,32 @@ from . import binding, operators, workloads
 STATE_BYTES = {32: 18, 8: 12}   # of an expert parameter on the GPU: copy, gradient, master and moments
 
 
-def router_forward(x, router, top_k):
+def router_forward(x, router, top_k, balance=None):
+    """The logits and the routing.  balance: None, or the arguments of a router whose choice is balanced: scores, bias,
+    groups, top_groups, group_best, scale (``operators.route_balanced``)."""
     logits = x @ router.T
-    return logits, operators.route(logits, top_k)
+    if balance is None:
+        return logits, operators.route(logits, top_k)
+    return logits, operators.route_balanced(logits, top_k, **balance)
 
 
-def router_backward(x, router, logits, routing, d_weight):
+def router_backward(x, router, logits, routing, d_weight, balance=None):
     """The gradients of the router's matrix and, through it, of x in fp32."""
-    d_logits = operators.route_backward(logits, routing, d_weight)
+    if balance is None:
+        d_logits = operators.route_backward(logits, routing, d_weight)
+    else:
+        d_logits = operators.route_balanced_backward(logits, routing, d_weight,
+                                                     **{k: balance[k] for k in ("scores", "scale") if k in balance})
     return d_logits.T @ x, (d_logits @ router).float()
 
 
-def layer_step(x, router, experts, d_out, top_k, mark=lambda name: None):
+def layer_step(x, router, experts, d_out, top_k, mark=lambda name: None, balance=None):
     """One layer forward and backward.  x [tokens, hidden], router [n_experts, hidden], experts: the gate, up
     and down matrices [n_experts, width, hidden], the same, [n_experts, hidden, width], d_out: the gradient of the
-    output.  Returns the routing, the output and the gradients; calls mark(name) where a part of the layer ends."""
+    output.  Returns the routing, the output and the gradients; calls mark(name) where a part of the layer ends.
+    balance as in ``router_forward``."""
     gate, up, down = experts
-    logits, r = router_forward(x, router, top_k)
+    logits, r = router_forward(x, router, top_k, balance)
     mark("route")
     g = operators.expert_matmul(x, gate, r.offset, slot=r.slot, top_k=top_k)
     u = operators.expert_matmul(x, up, r.offset, slot=r.slot, top_k=top_k)
@@ -63,17 +74,39 @@ def layer_step(x, router, experts, d_out, top_k, mark=lambda name: None):
     mark("experts")
     d_x = operators.combine(d_rows[0], r.place).float() + operators.combine(d_rows[1], r.place).float()
     mark("combine")
-    d_router, d_rest = router_backward(x, router, logits, r, d_weight)
+    d_router, d_rest = router_backward(x, router, logits, r, d_weight, balance)
     d_x += d_rest
     mark("route")
     return {"routing": r, "out": out, "d_x": d_x.to(x.dtype), "d_router": d_router,
             "d_experts": (d_gate, d_up, d_down)}
 
 
+def block_step(token, table, norm, router, experts, d_out, top_k, drop, grad, mark=lambda name: None, balance=None):
+    """A layer in its place, forward and backward: out = x + dropout(layer(norm(x))), x = the token's rows of table.
+
+    token [tokens], table [vocab, hidden], norm: the norm's weight and bias, drop: (p, seed, offset) of the dropout, grad
+    [vocab, hidden] fp32: the table's gradient, which this step's is added to; the rest as in ``layer_step``, whose
+    result comes with the block's output, the gradient of x and those of the norm."""
+    x = operators.embed(token, table)
+    mark("embed")
+    n, mean, rstd = operators.layer_norm(x, *norm)
+    mark("norm")
+    d_layer = operators.dropout_backward(d_out, *drop)
+    mark("dropout")
+    got = layer_step(n, router, experts, d_layer, top_k, mark, balance)
+    out = operators.dropout(got["out"], *drop, residual=x)
+    mark("dropout")
+    d_x, d_norm, d_norm_bias = operators.layer_norm_backward(got["d_x"], x, norm[0], mean, rstd, add=d_out)
+    mark("norm")
+    operators.embed_backward(d_x, token, table.shape[0], into=grad)
+    mark("embed")
+    return dict(got, out=out, d_x=d_x, d_norm=(d_norm, d_norm_bias), d_table=grad)
+
+
 class Layer:
     """The layer's weights, AdamW state and inputs on the current device, random."""
 
-    def __init__(self, tokens, hidden, width, n_experts, top_k, state_bits=32, skew=1.1, seed=0):
+    def __init__(self, tokens, hidden, width, n_experts, top_k, state_bits=32, skew=1.1, seed=0, balance=None):
         gen = torch.Generator(device="cuda").manual_seed(seed)
 
         def normal(*shape, scale=1.0, dtype=torch.bfloat16):
@@ -82,7 +115,7 @@ class Layer:
                 part.copy_(torch.randn(part.numel(), generator=gen, device="cuda") * scale)
             return out
 
-        self.top_k = top_k
+        self.top_k, self.balance = top_k, balance
         shapes = [(n_experts, width, hidden)] * 2 + [(n_experts, hidden, width)]
         self.masters = [normal(*s, scale=s[2] ** -0.5, dtype=torch.float32) for s in shapes]
         self.experts = [m.bfloat16() for m in self.masters]
@@ -102,24 +135,49 @@ class Layer:
         self.optimizer = operators.AdamW(self.masters, m, v, copies=self.experts, weight_decay=0.1, **small)
         self.steps = 0
 
+    def forward_backward(self, mark):
+        return layer_step(self.x, self.router, self.experts, self.d_out, self.top_k, mark, self.balance)
+
     def step(self, mark=lambda name: None):
         """A training step; the optimizer's part is marked "optimizer"."""
-        got = layer_step(self.x, self.router, self.experts, self.d_out, self.top_k, mark)
+        got = self.forward_backward(mark)
         self.steps += 1
         self.optimizer.step(got["d_experts"], lr=1e-4, step=self.steps, seed=self.steps)
         mark("optimizer")
         return got
 
 
-def _router_step(tokens, hidden, experts, top_k, seed):
+class Block(Layer):
+    """The layer in its place, with a norm, an embedding of ``vocab`` tokens, words' shares, and a dropout of chance p."""
+
+    def __init__(self, tokens, hidden, width, n_experts, top_k, state_bits=32, skew=1.1, seed=0, balance=None, vocab=32768,
+                 p=0.1):
+        super().__init__(tokens, hidden, width, n_experts, top_k, state_bits, skew, seed, balance)
+        gen = torch.Generator(device="cuda").manual_seed(seed + 1)
+        share = 1.0 / torch.arange(1, vocab + 1, device="cuda", dtype=torch.float64)
+        edges = (share / share.sum()).cumsum(0)
+        u = torch.rand(tokens, generator=gen, device="cuda", dtype=torch.float64)
+        self.token = torch.searchsorted(edges, u).clamp_max(vocab - 1)
+        self.table = torch.randn((vocab, hidden), generator=gen, device="cuda").bfloat16()
+        self.norm = torch.ones(hidden, device="cuda"), torch.zeros(hidden, device="cuda")
+        self.grad = torch.zeros((vocab, hidden), device="cuda")
+        self.p, self.seed = p, seed
+
+    def forward_backward(self, mark):
+        # another mask for every step
+        return block_step(self.token, self.table, self.norm, self.router, self.experts, self.d_out, self.top_k,
+                          (self.p, self.seed, self.steps), self.grad, mark, self.balance)
+
+
+def _router_step(tokens, hidden, experts, top_k, seed, balance=None):
     """The router of a layer of this size, forward and backward, by itself."""
     layer = Layer(tokens, hidden, 1, experts, top_k, seed=seed)
     d_weight = torch.ones((tokens, top_k), device="cuda")
     d_x = torch.zeros((tokens, hidden), device="cuda")
 
     def step(mark):
-        logits, r = router_forward(layer.x, layer.router, top_k)
-        _, d_rest = router_backward(layer.x, layer.router, logits, r, d_weight)
+        logits, r = router_forward(layer.x, layer.router, top_k, balance)
+        _, d_rest = router_backward(layer.x, layer.router, logits, r, d_weight, balance)
         d_x.add_(d_rest)
         mark("route")
     return step
@@ -148,13 +206,17 @@ def _times(step, warmup, steps):
     return got, {name: sorted(v)[len(v) // 2] for name, v in spent.items()}
 
 
-def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=100 * 10**9, seed=0):
+def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=100 * 10**9, seed=0, balance=None, vocab=0):
     """Time the MoE layer ``layer`` (the first, if None) of a problem's model on the current device.
 
     Where all its experts do not fit ``limit_bytes``, an equal part of them takes an equal part of the tokens and
     the times of the experts and of the rows' sum count for the whole; the router, whose work is tokens times experts,
     then runs by itself at its whole size (by equal parts of its experts, where they are more than it takes).  Returns
-    ns of the parts for one micro-batch, forward and backward, the optimizer's ns a parameter and the router's counts."""
+    ns of the parts for one micro-batch, forward and backward, the optimizer's ns a parameter and the router's counts.
+
+    balance: as in ``router_forward``; of a bias of all experts, those that run have the first entries.  vocab: not 0, the layer runs
+    in its place (``block_step``), with an embedding of that many tokens, and the ns of embedding, norm and dropout come
+    too."""
     m = problem["model"]
     moe = [i for i in range(m["n_layers"]) if m["is_moe"][i]]
     if not moe:
@@ -169,16 +231,24 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
     while experts // part * 3 * width * hidden * STATE_BYTES[state_bits] > limit_bytes and \
             experts % (2 * part) == 0 and experts // (2 * part) >= top_k and tokens % (2 * part) == 0:
         part *= 2
-    run = Layer(tokens // part, hidden, width, experts // part, top_k, state_bits, seed=seed)
+    def of(n):   # the balance of the first n experts
+        if balance is None or balance.get("bias") is None:
+            return balance
+        return dict(balance, bias=balance["bias"][:n])
+
+    size = tokens // part, hidden, width, experts // part, top_k, state_bits
+    how = {"seed": seed, "balance": of(experts // part)}
+    run = Block(*size, vocab=vocab, **how) if vocab else Layer(*size, **how)
     got, ns = _times(run.step, warmup, steps)
     route_ns = ns["route"]
     if part > 1:
         cut = 1   # where the router cannot take all experts at once
         while experts // cut > operators.MAX_EXPERTS:
             cut *= 2
-        route_ns = _times(_router_step(tokens, hidden, experts // cut, top_k, seed), warmup, steps)[1]["route"] * cut
+        route_ns = _times(_router_step(tokens, hidden, experts // cut, top_k, seed, of(experts // cut)), warmup, steps)[1]["route"] * cut
     params = experts // part * 3 * width * hidden
-    return {"layer": layer, "tokens": tokens, "hidden": hidden, "width": width, "experts": experts, "part": part,
+    around = {f"{name}_ns": ns[name] * part for name in ("embed", "norm", "dropout") if name in ns}
+    return {**around, "layer": layer, "tokens": tokens, "hidden": hidden, "width": width, "experts": experts, "part": part,
             "route_ns": route_ns, "combine_ns": ns["combine"] * part, "experts_ns": ns["experts"] * part,
             "opt_ns_per_param": ns["optimizer"] / params,
             "expert_tokens": got["routing"].count.cpu().numpy().astype(np.int64)}
@@ -223,15 +293,24 @@ def main(argv=None):
     p.add_argument("--type", type=int, default=0, help="device type that this GPU stands for")
     p.add_argument("--state-bits", type=int, default=32, choices=(8, 32))
     p.add_argument("--steps", type=int, default=5)
+    p.add_argument("--scores", choices=sorted(operators.SCORES), help="a router whose choice is balanced, by these scores")
+    p.add_argument("--groups", type=int, default=1, help="its groups of experts")
+    p.add_argument("--top-groups", type=int, help="those that stay; none given: all")
+    p.add_argument("--block", action="store_true", help="the layer with its embedding, norm and dropout")
+    p.add_argument("--vocab", type=int, default=32768, help="tokens of the embedding")
     a = p.parse_args(argv)
     problem = workloads.config(a.config)
-    got = measure(problem, steps=a.steps, state_bits=a.state_bits)
+    balance = a.scores and {"scores": a.scores, "groups": a.groups, "top_groups": a.top_groups}
+    got = measure(problem, steps=a.steps, state_bits=a.state_bits, balance=balance, vocab=a.vocab if a.block else 0)
     print(f"layer {got['layer']}: {got['tokens']} tokens, hidden {got['hidden']}, {got['experts']} experts of width "
           f"{got['width']}" + (f", one of {got['part']} parts run" if got["part"] > 1 else ""))
     flops = 3 * 6.0 * got["tokens"] * int(problem["model"]["top_k"]) * got["hidden"] * got["width"]
     print(f"experts {got['experts_ns'] / 1e3:.0f} us ({flops / got['experts_ns'] / 1e3:.0f} TFLOP/s), router "
           f"{got['route_ns'] / 1e3:.0f} us, rows' sum {got['combine_ns'] / 1e3:.0f} us, optimizer "
           f"{got['opt_ns_per_param'] * 1e3:.2f} ps a parameter")
+    if a.block:
+        print(f"embedding {got['embed_ns'] / 1e3:.0f} us, norm {got['norm_ns'] / 1e3:.0f} us, dropout "
+              f"{got['dropout_ns'] / 1e3:.0f} us")
     for name, q in (("as given", problem), ("measured", apply(problem, a.type, got, counts=False))):
         plan = binding.Planner(q, "cuda:0").run()
         print(f"{name}: (PP, TP, CP, DP, EP, TPE) {plan['config']}, B {plan['n_micro']}, {plan['objective']} ns, layers "

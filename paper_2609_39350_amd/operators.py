@@ -141,6 +141,9 @@ def _array(name, t, dtype, *shape):
 
 def _matrix(name, t, types):
     """A matrix of one of the types whose rows are contiguous; the distance of its rows in elements."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.dim() == 2 and t.is_contiguous() \
+            and t.get_device() == _device() and t.shape[1]:
+        return t.shape[1]
     _on_device(name, t)
     if t.dtype not in types:
         raise ValueError(f"{name}: one of {', '.join(str(x) for x in types)}, not {t.dtype}")
@@ -415,7 +418,10 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
 
 # ----------------------------------------------------------- around the layer
 def _vector(name, t, types, n):
-    """A contiguous vector of n elements of one of the types."""
+    """A contiguous vector of n elements (None: any) of one of the types."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.dim() == 1 and t.shape[0] == (t.shape[0] if n is None
+            else n) and t.is_contiguous() and t.get_device() == _device():
+        return
     _on_device(name, t)
     if t.dtype not in types:
         raise ValueError(f"{name}: one of {', '.join(str(x) for x in types)}, not {t.dtype}")
