@@ -302,18 +302,20 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
 #pragma unroll
             for (int c = 0; c < PER; ++c) v[c] = v[c] == kClosed ? kClosed : key_of(x[c]);
         }
-        wave_order();   // the keys before are read
+        if constexpr (keys_in_lds(PER)) {
+            wave_order();   // the keys before are read
 #pragma unroll
-        for (int c = 0; c < PER; c += 4)
-            *reinterpret_cast<int4 *>(row + lane * PER + c) = make_int4(v[c], v[c + 1], v[c + 2], v[c + 3]);
-        wave_order();
+            for (int c = 0; c < PER; c += 4)
+                *reinterpret_cast<int4 *>(row + lane * PER + c) = make_int4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+            wave_order();
+        }
         int own = lane_largest<int, PER>(v), most = row_reduce(own, Max());
         int who[2] = {-1, -1};   // choices lane and lane + 16
         int before = -1;         // the choice before, where this one is near to it
         for (int j = 0; j <= top_k && most != kClosed && (j < top_k || before >= 0); ++j) {
-            const int from = first_of_row(own == most);
             int best;
-            if constexpr (PER >= 16) {
+            if constexpr (keys_in_lds(PER)) {
+                const int from = first_of_row(own == most);
                 int k[PER / 16], at = 0;
 #pragma unroll
                 for (int i = 0; i < PER / 16; ++i) k[i] = row[from * PER + 16 * i + lane];
@@ -330,13 +332,14 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
                 const int left = row_reduce(lane_largest<int, PER / 16>(k), Max());
                 own = lane == from ? left : own;
             } else {
-                const int k = lane < PER ? row[from * PER + lane] : kClosed;
-                const int at = first_of_row(k == most);
-                best = from * PER + at;
-                if (lane == 0) row[best] = kClosed;
-                wave_order();
-                const int left = row_reduce(lane == at ? kClosed : k, Max());
-                own = lane == from ? left : own;
+                int at = PER;
+#pragma unroll
+                for (int c = PER - 1; c >= 0; --c) at = v[c] == most ? c : at;
+                best = row_reduce(at < PER ? lane * PER + at : INT32_MAX, Min());
+                const int mine = best - lane * PER;
+#pragma unroll
+                for (int c = 0; c < PER; ++c) v[c] = c == mine ? kClosed : v[c];
+                own = lane_largest<int, PER>(v);
             }
             // equal logits and biases have equal sums, however near; others may not be in this order
             if (before >= 0)
@@ -347,13 +350,26 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
             most = row_reduce(own, Max());
             before = q.bias && most != kClosed && !(value - logit_of(most) > error + kUnit / 2 * fabsf(value)) ? best : -1;
         }
-        // Of up to 15 choices and the first that is not, where it is near to the last, sigmoids in 64 bits are one a lane: they
-        // are put in order here.  All else that is near takes a wave; so does an expert that is near to the first not chosen.
-        again = again || before >= 0 || (near && (!SIGMOID || top_k > 15));
-        if (SIGMOID && __ballot(near && !again)) {
+        // Up to 15 choices and the first that is not, where it is near to the last, are one a lane: they are put in order here,
+        // by their scores in 64 bits.  All else that is near takes a wave; so does an expert near to the first not chosen.
+        again = again || before >= 0 || (near && top_k > 15);
+        if (__ballot(near && !again)) {
+            double all = 0.0;   // of a softmax
+            if constexpr (!SIGMOID) {
+#pragma unroll 1
+                for (int c = lane * PER; c < min(lane * PER + PER, experts); ++c) {
+                    const float y = to_f32(logits[c]);
+                    all += y > -INFINITY && top > -INFINITY ? exp(y == top ? 0.0 : (double)y - (double)top) : 0.0;
+                }
+                all = row_reduce(all, Sum());
+            }
             const int e = who[0];
             double sum = -INFINITY;
-            if (e >= 0) sum = 1.0 / (1.0 + exp(-(double)to_f32(logits[e]))) + (double)(q.bias ? q.bias[e] : 0.0f);
+            if (e >= 0) {
+                const float y = to_f32(logits[e]);
+                const double power = exp(SIGMOID ? -(double)y : y == top ? 0.0 : (double)y - (double)top);
+                sum = (SIGMOID ? 1.0 : power) / (SIGMOID ? 1.0 + power : all) + (double)(q.bias ? q.bias[e] : 0.0f);
+            }
             int rank = 0, other_e = e;
             double other = sum;
 #pragma unroll 1

@@ -214,9 +214,9 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
     then runs by itself at its whole size (by equal parts of its experts, where they are more than it takes).  Returns
     ns of the parts for one micro-batch, forward and backward, the optimizer's ns a parameter and the router's counts.
 
-    balance: as in ``router_forward``; of a bias of all experts, those that run have the first entries.  vocab: not 0, the layer runs
-    in its place (``block_step``), with an embedding of that many tokens, and the ns of embedding, norm and dropout come
-    too."""
+    balance: as in ``router_forward``; of a bias of all experts, those that run have the first entries.  vocab: not 0,
+    the layer runs in its place (``block_step``), with an embedding of that many tokens, and the ns of embedding, norm and
+    dropout come too."""
     m = problem["model"]
     moe = [i for i in range(m["n_layers"]) if m["is_moe"][i]]
     if not moe:
@@ -245,7 +245,8 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
         cut = 1   # where the router cannot take all experts at once
         while experts // cut > operators.MAX_EXPERTS:
             cut *= 2
-        route_ns = _times(_router_step(tokens, hidden, experts // cut, top_k, seed, of(experts // cut)), warmup, steps)[1]["route"] * cut
+        alone = _router_step(tokens, hidden, experts // cut, top_k, seed, of(experts // cut))
+        route_ns = _times(alone, warmup, steps)[1]["route"] * cut
     params = experts // part * 3 * width * hidden
     around = {f"{name}_ns": ns[name] * part for name in ("embed", "norm", "dropout") if name in ns}
     return {**around, "layer": layer, "tokens": tokens, "hidden": hidden, "width": width, "experts": experts, "part": part,

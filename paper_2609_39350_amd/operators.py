@@ -419,8 +419,8 @@ def expert_matmul_grad_w(d_y, x, offset, slot=None, top_k=1, dtype=torch.float32
 # ----------------------------------------------------------- around the layer
 def _vector(name, t, types, n):
     """A contiguous vector of n elements (None: any) of one of the types."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.dim() == 1 and t.shape[0] == (t.shape[0] if n is None
-            else n) and t.is_contiguous() and t.get_device() == _device():
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in types and t.dim() == 1 and (n is None or t.shape[0] == n) \
+            and t.is_contiguous() and t.get_device() == _device():
         return
     _on_device(name, t)
     if t.dtype not in types:
