@@ -177,6 +177,48 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const void *__restrict__ 
     }
 }
 
+// The same order by counting: a place's is the number of places of lower tokens and of earlier ones of its own.  A
+// workgroup counts for 16 places of a segment, each of its threads for one of them over a 64th of the segment's, four at a
+// time out of LDS: so that a few thousand places are all CUs' work and not one's.
+constexpr int kRanked = 16;
+template <typename I>
+__global__ __launch_bounds__(kSortThreads) void k_rank(const void *__restrict__ token, int64_t tokens, int64_t vocab,
+                                                       int2 *__restrict__ sorted)
+{
+    __shared__ __attribute__((aligned(16))) int key[kSegment];
+    __shared__ int part[kSortWaves][kRanked];
+    constexpr int kGroups = kSegment / kRanked;
+    const int64_t first = (int64_t)(blockIdx.x / kGroups) * kSegment;
+    const int n = tokens - first < kSegment ? (int)(tokens - first) : kSegment, i0 = blockIdx.x % kGroups * kRanked;
+    if (i0 >= n) return;
+    const int fours = (n + 3) / 4;
+    for (int i = threadIdx.x; i < fours * 4; i += kSortThreads) {
+        const int64_t v = i < n ? token_at<I>(token, first + i) : 0;
+        key[i] = i >= n ? INT32_MAX : (uint64_t)v < (uint64_t)vocab ? (int)v : (int)vocab;   // behind all: counted by none
+    }
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, i = i0 + (threadIdx.x & 15);
+    const int mine = i < n ? key[i] : 0;
+    int count = 0;
+    for (int f = threadIdx.x >> 4; f < fours; f += kSortThreads / 16) {
+        const int4 k = reinterpret_cast<const int4 *>(key)[f];
+        const int below = mine + (f * 4 + 3 < i ? 1 : 0);   // equal ones count where they are earlier
+        count += (k.x < below) + (k.y < below) + (k.z < below) + (k.w < below);
+    }
+    if ((threadIdx.x >> 4) == 0 && i < n)   // and those in the place's own four
+        for (int j = i & ~3; j < i; ++j) count += key[j] == mine;
+    count += __shfl_xor(count, 16, 64);
+    count += __shfl_xor(count, 32, 64);
+    if ((threadIdx.x & 63) < kRanked) part[wave][threadIdx.x & 63] = count;
+    __syncthreads();
+    if (threadIdx.x < kRanked && i < n) {
+        int at = 0;
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) at += part[w][threadIdx.x];
+        sorted[first + at] = make_int2(mine, (int)first + i);
+    }
+}
+
 // Runs of `run` sorted places each -> runs of kWays * run: a place goes behind its own run's earlier ones and, of every
 // other run, those of lower tokens, and of the runs before its own those of the same token too.  A search begins in
 // kSamples places of each run, out of LDS: 17 us for 32,768 places with all of its steps out of the cache.
@@ -323,31 +365,35 @@ __global__ __launch_bounds__(kThreads) void k_embed_sum(const T *__restrict__ d_
     }
 }
 
-// The token that begins in chunk `workgroup` and goes on: its sums there and in the chunks that follow, a run of them for
-// each quarter of the workgroup, then the quarters in their order.
+// The token that begins in a chunk and goes on: its sums there and in the chunks that follow, a run of them for each
+// quarter of the workgroup, then the quarters in their order.
 constexpr int kJoinThreads = 1024, kQuarters = kJoinThreads / kThreads;
 __global__ __launch_bounds__(kJoinThreads) void k_embed_join(int hidden, const int2 *__restrict__ sorted, int64_t n,
-                                                             int chunk, int vocab, float scale, bool add,
+                                                             int chunk, int lanes, int vocab, float scale, bool add,
                                                              const float *__restrict__ part, float *__restrict__ d_table)
 {
     constexpr int kAhead = 8;
     __shared__ float sh[kQuarters - 1][8][kThreads];
-    const int64_t which = workgroup(), lo = which * chunk, hi = lo + chunk;
-    if (hi >= n) return;
-    const int token = sorted[hi - 1].x;
-    if (token == vocab || sorted[hi].x != token || (lo > 0 && sorted[lo - 1].x == token)) return;
-    int64_t chunks = 0;   // behind this one that begin with the token
-    for (int64_t a = 0, b = (n - hi + chunk - 1) / chunk; a < b;) {
-        const int64_t half = (a + b) >> 1;
-        if (sorted[hi + half * chunk].x == token)
-            a = half + 1;
-        else
-            b = half;
-        chunks = a;
-    }
     const int thread = threadIdx.x % kThreads, quarter = threadIdx.x / kThreads;
-    const Columns c(hidden, blockIdx.y * kThreads + thread);
-    const bool has = c.skip < 8;
+    const int64_t which = workgroup() * (kThreads / lanes) + thread / lanes, lo = which * chunk, hi = lo + chunk;
+    const Columns c(hidden, blockIdx.y * lanes + thread % lanes);
+    int token = vocab;
+    if (hi < n && c.skip < 8) {
+        token = sorted[hi - 1].x;
+        if (sorted[hi].x != token || (lo > 0 && sorted[lo - 1].x == token)) token = vocab;
+    }
+    const bool has = token != vocab;
+    if (!__syncthreads_or(has)) return;
+    int64_t chunks = 0;   // behind this one that begin with the token
+    if (has)
+        for (int64_t a = 0, b = (n - hi + chunk - 1) / chunk; a < b;) {
+            const int64_t half = (a + b) >> 1;
+            if (sorted[hi + half * chunk].x == token)
+                a = half + 1;
+            else
+                b = half;
+            chunks = a;
+        }
     // sum 0 is this chunk's, sum i of the chunk i behind it
     const int64_t each = (chunks + kQuarters) / kQuarters, first = min(quarter * each, chunks + 1);
     const int64_t last = min(first + each, chunks + 1);
@@ -414,9 +460,18 @@ __global__ __launch_bounds__(kThreads) void k_embed_narrow(const T *__restrict__
         if (j < hidden) d_table[row * hidden + j] = (add ? d_table[row * hidden + j] : 0.0f) + sum[j] * scale;
 }
 
-// Places of a chunk.  us by 32, 64, 128: 32,768 places: 131,072 x 4,096, tokens as words fall 535, 516, 547, all of one token 641,
-// 562, 548; 1,000 x 7,168 177, 160, 155 and 284, 194, 163.  Few places need many chunks.
-int chunk_of(int64_t tokens) { return tokens < 8192 ? 8 : tokens < 65536 ? 64 : kChunkMost; }
+// Up to this many places are sorted by counting.  us of a call of 64 columns by counting, by digits: 1,000 places 13.3, 13.6 (the
+// host's), 4,096 16.1, 22.7, 8,192 49, 55, 16,384 54, 56, 32,768 66, 58.
+constexpr int64_t kRankMost = 16384;
+
+// Places of a chunk: the most that leave two workgroups a CU, if any do.  us by 64, 128: 32,768 places: 131,072 x 4,096, tokens
+// as words fall 513, 527, all of one token 559, 524; 32,768 x 4,096 230, 222 and 273, 228; 1,000 x 7,168 170, 154 and 194, 159.
+int chunk_of(int64_t tokens, int64_t hidden)
+{
+    int chunk = kRowsAhead;
+    while (chunk < kChunkMost && ceil_div(tokens, 2 * chunk) * ceil_div(hidden, 8) >= 512 * kThreads) chunk *= 2;
+    return chunk;
+}
 
 template <typename F>
 hipError_t by_type(int type, F f)
@@ -432,7 +487,7 @@ hipError_t by_type(int type, F f)
 int64_t embed_ws_bytes(int64_t tokens, int64_t hidden)
 {
     const int64_t places = ceil_div(tokens, 2) * 16;
-    return (tokens > kSegment ? 2 : 1) * places + ceil_div(tokens, chunk_of(tokens)) * 2 * hidden * 4;
+    return (tokens > kSegment ? 2 : 1) * places + ceil_div(tokens, chunk_of(tokens, hidden)) * 2 * hidden * 4;
 }
 
 hipError_t launch_embed(const void *token, bool wide, int64_t tokens, const void *table, int type, int64_t stride,
@@ -466,16 +521,21 @@ hipError_t launch_embed_backward(const void *d_out, int type, int64_t stride, in
     float *part = reinterpret_cast<float *>(tokens > kSegment ? other + places : other);
     int bits = 1;
     while (vocab >> bits) ++bits;
-    if (tokens > 0)
+    if (tokens > kRankMost)
         hipLaunchKernelGGL((wide ? k_sort<int64_t> : k_sort<int32_t>), dim3((unsigned)ceil_div(tokens, kSegment)),
                            dim3(kSortThreads), 0, s, token, tokens, vocab, bits, sorted);
+    else if (tokens > 0)
+        hipLaunchKernelGGL((wide ? k_rank<int64_t> : k_rank<int32_t>),
+                           dim3((unsigned)(tokens > kSegment ? ceil_div(tokens, kSegment) * (kSegment / kRanked)
+                                                             : ceil_div(tokens, kRanked))),
+                           dim3(kSortThreads), 0, s, token, tokens, vocab, sorted);
     for (int64_t run = kSegment; run < tokens; run *= kWays) {
         hipLaunchKernelGGL(k_merge, many(ceil_div(tokens, kThreads)), dim3(kThreads), 0, s, sorted, other, (int)tokens,
                            (int)run);
         int2 *const t = sorted;
         sorted = other, other = t;
     }
-    const int chunk = chunk_of(tokens), lanes = lanes_of(hidden);
+    const int chunk = chunk_of(tokens, hidden), lanes = lanes_of(hidden);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
         const T *d = static_cast<const T *>(d_out);
@@ -494,8 +554,8 @@ hipError_t launch_embed_backward(const void *d_out, int type, int64_t stride, in
                            dim3(kThreads), lds > kThreads * 4 ? lds : kThreads * 4, s, d, stride, (int)hidden, sorted,
                            tokens, chunk, lanes, (int)vocab, scale, d_table, part, sums, (int)rows_each);
         if (chunks > 1)
-            hipLaunchKernelGGL(k_embed_join, many(chunks - 1, (unsigned)ceil_div(hidden, 8 * kThreads)),
-                               dim3(kJoinThreads), 0, s, (int)hidden, sorted, tokens, chunk, (int)vocab, scale, add, part, d_table);
+            hipLaunchKernelGGL(k_embed_join, many(ceil_div(chunks - 1, kThreads / lanes), columns), dim3(kJoinThreads), 0, s,
+                               (int)hidden, sorted, tokens, chunk, lanes, (int)vocab, scale, add, part, d_table);
         return hipGetLastError();
     });
 }
