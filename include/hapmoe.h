@@ -680,7 +680,7 @@ int32_t hapmoe_embed_ws_bytes(int64_t tokens, int64_t hidden, int64_t *bytes);
 /* The table's gradient, fp32: row v = scale * sum of d_out[t] over the t with
  * token[t] = v.  add = 0: d_d_table [vocab][hidden] is written whole, rows
  * without a token 0; else it is added to d_d_table, rows without a token are
- * left as they are.  Each row's order of the sum is fixed. */
+ * left as they are.  Each row's order of the sum is fixed.  vocab < 2^31 - 1. */
 int32_t hapmoe_embed_backward(const void *d_d_out, int32_t type, int64_t stride, int64_t tokens, int64_t hidden,
                               const void *d_token, int32_t token_bits, int64_t vocab, float scale, int32_t add,
                               float *d_d_table, void *d_ws, int64_t ws_bytes, void *stream);

@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void k_merge(const int2 *__restrict__ fro
         for (int half = kSamples / 2; half > 0; half >>= 1) c += sample[w][c + half - 1] <= key ? half : 0;
         c += sample[w][c] <= key ? 1 : 0;
         lo[w] = begin(w) + (c > 0 ? (c - 1) * step + 1 : 0);
-        size[w] = begin(w) == mine || c == 0 ? 0 : max(min(begin(w) + c * step, begin(w + 1)) - lo[w], 0);
+        size[w] = begin(w) == mine || c == 0 ? 0 : max((int)min(begin(w) + (int64_t)c * step, (int64_t)begin(w + 1)) - lo[w], 0);
     }
     for (int most = step; most > 0; most >>= 1) {   // all runs' searches side by side
         int other[kWays];

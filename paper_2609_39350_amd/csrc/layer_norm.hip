@@ -448,7 +448,10 @@ int64_t workgroups_of(Share sh, int64_t rows, int a_cu)
 int parts_of(int64_t rows, int64_t hidden)
 {
     const Share sh = share_of(hidden);
-    return (int)(sh.threads ? workgroups_of(sh, rows, kBackward) : rows < 512 ? rows : 512);
+    if (sh.threads) return (int)workgroups_of(sh, rows, kBackward);
+    int64_t most = (int64_t)2048 * kThreads / hidden;   // of long rows few: the columns fill the card
+    most = most < 1 ? 1 : most > 512 ? 512 : most;
+    return (int)(rows < most ? rows : most);
 }
 
 template <typename F>

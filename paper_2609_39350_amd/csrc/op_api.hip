@@ -338,6 +338,7 @@ int32_t hapmoe_embed_backward(const void *d_d_out, int32_t type, int64_t stride,
                               float *d_d_table, void *d_ws, int64_t ws_bytes, void *stream)
 {
     if (!any_type(type) || bad_rows(tokens, hidden, stride) || bad_rows(vocab, hidden, hidden) || vocab < 1 ||
+        vocab > INT32_MAX - 1 ||   // a token that is none of the table's sorts as vocab, before the end's mark
         (token_bits != 32 && token_bits != 64) || !std::isfinite(scale))
         return HAPMOE_E_INVAL;
     if (!d_d_table || !aligned(d_d_table, 4) || (tokens > 0 && (!d_d_out || !d_token))) return HAPMOE_E_INVAL;

@@ -403,7 +403,7 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
     __syncthreads();
     // the tokens that are left, a wave for each in turn
     int number = 0;
-    uint64_t left = __ballot(wave_lane < here && chosen[min(wave_lane, here - 1) * top_k] == kAgain);
+    uint64_t left = __ballot(wave_lane < here && chosen[wave_lane * top_k] == kAgain);
     __syncthreads();   // every wave has them before the first is replaced
     for (; left; left &= left - 1) {
         if (number++ % kWaves != (int)(threadIdx.x >> 6)) continue;

@@ -503,8 +503,8 @@ def embed_backward(d_out, token, vocab: int, scale=1.0, into=None):
     stride = _matrix("d_out", d_out, _TYPES)
     tokens, hidden = d_out.shape
     _vector("token", token, _TOKEN_BITS, tokens)
-    if not 1 <= vocab < 2**31:
-        raise ValueError(f"vocab: at least 1 and below 2^31, not {vocab}")
+    if not 1 <= vocab < 2**31 - 1:
+        raise ValueError(f"vocab: at least 1 and below 2^31 - 1, not {vocab}")
     if into is None:
         d_table = torch.empty((vocab, hidden), dtype=torch.float32, device=d_out.device)
     else:

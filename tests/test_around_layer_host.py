@@ -48,6 +48,8 @@ def test_layer_norm():
     need = C.c_int64(-1)
     assert L.hapmoe_layer_norm_ws_bytes(0, 128, C.byref(need)) == 0 and need.value == 0
     assert L.hapmoe_layer_norm_ws_bytes(64, 128, C.byref(need)) == 0 and need.value > 0
+    for long in (20000, 2**24):   # rows that no workgroup holds: the workspace stays small
+        assert L.hapmoe_layer_norm_ws_bytes(4096, long, C.byref(need)) == 0 and 0 < need.value <= max(2**23, 8 * long)
     for bad in ((-1, 128), (64, 0), (64, 2**25), (2**31, 8)):
         assert L.hapmoe_layer_norm_ws_bytes(*bad, C.byref(need)) == INVAL
     assert L.hapmoe_layer_norm_ws_bytes(64, 128, None) == INVAL
@@ -78,7 +80,7 @@ def test_embed():
     f = L.hapmoe_embed_backward
     refuses(f, good, {
         0: (None, P + 2), 1: (-1, 3), 2: (127,), 3: (-1, 2**31), 4: (0, 2**25), 5: (None, P + 4), 6: (8,),
-        7: (0, 2**31), 8: (math.nan,), 10: (None, P + 2), 11: (None, P + 8)})
+        7: (0, 2**31, 2**31 - 1), 8: (math.nan,), 10: (None, P + 2), 11: (None, P + 8)})
     assert f(*changed(good, a12=16)) == WORKSPACE
 
 

@@ -75,7 +75,7 @@ def test_sizes_and_numbers():
         refused(ops.embed, token, x, scale=scale)
         refused(ops.embed_backward, x, token, 9, scale=scale)
     refused(ops.embed, token.short(), x)
-    for vocab in (0, -1, 2**31, 2**32 + 9):
+    for vocab in (0, -1, 2**31 - 1, 2**31, 2**32 + 9):
         refused(ops.embed_backward, x, token, vocab)
     refused(ops.embed_backward, x, token, 9, into=torch.zeros(9, 16, device="cuda", dtype=torch.bfloat16))
     for p in (-0.1, 1.5, math.nan):
