@@ -2,12 +2,17 @@
 //
 // out[t] = scale table[token[t]], a row of zeros where the token is none of the table's.
 //
-// The gradient's row of a token is the sum over its places in the order of t, with no atomics.  Workgroups sort up to
-// 4,096 places each by token in LDS: a stable counting sort, up to 9 bits of the token a pass; a launch puts up to 16
-// such segments into one order, every place by a search in each of the others.  Then workgroups take equal chunks of the
-// sorted places, whatever the tokens' shares: a token that lies within a chunk is written, one that goes on into the
-// next leaves its sums in the workspace, and a last launch puts those together.  Rows without a token are cleared by
+// The gradient's row of a token is the sum over its places in a fixed order, with no atomics.  The places are put in the
+// tokens' order by segments of 4,096, few by counting for each place those before it, many by a stable sort of 9 bits a
+// pass in LDS; a launch puts up to 16 segments into one order, every place by a search in each of the others.  Then
+// workgroups take equal chunks of the sorted places, whatever the tokens' shares: a token that lies within a chunk is
+// written, one that goes on into the next leaves its sums in the workspace, and a last launch puts those together.  Rows without a token are cleared by
 // further workgroups of the same launch, which look for them in the sorted places.
+//
+// Bound by HBM where the table's gradient is written whole, by launches that wait for each other where few rows are added
+// to.  bf16, 32,768 places, tokens as words fall, of 131,072 x 4,096: forward 77 us (0.38 GB, 5.0 TB/s), sort 12, segments
+// together 14, sums and clears 455 (2.4 GB, 5.3 TB/s; a fill of as much takes 5.4 to 6.8), what goes on 14.  4,001
+// places of 1,023 fp16 added to: 4.8 forward, then 5.3, 8.0 and 7.6.
 #include "operators.h"
 
 namespace hapmoe {
@@ -65,7 +70,8 @@ __global__ __launch_bounds__(kThreads) void k_embed(const void *__restrict__ tok
     const int64_t v = token_at<I>(token, t);
     const bool real = (uint64_t)v < (uint64_t)vocab;
     if (LANES == 0 && hidden < 8) {
-        for (int h = 0; h < hidden; ++h) out[t * hidden + h] = from_f32<T>(real ? to_f32(table[v * stride + h]) * scale : 0.0f);
+        for (int h = 0; h < hidden; ++h)
+            out[t * hidden + h] = from_f32<T>(real ? to_f32(table[v * stride + h]) * scale : 0.0f);
         return;
     }
     const Columns c(hidden, blockIdx.y * lanes + threadIdx.x % lanes);
@@ -249,7 +255,8 @@ __global__ __launch_bounds__(kThreads) void k_merge(const int2 *__restrict__ fro
         for (int half = kSamples / 2; half > 0; half >>= 1) c += sample[w][c + half - 1] <= key ? half : 0;
         c += sample[w][c] <= key ? 1 : 0;
         lo[w] = begin(w) + (c > 0 ? (c - 1) * step + 1 : 0);
-        size[w] = begin(w) == mine || c == 0 ? 0 : max((int)min(begin(w) + (int64_t)c * step, (int64_t)begin(w + 1)) - lo[w], 0);
+        const int end = (int)min(begin(w) + (int64_t)c * step, (int64_t)begin(w + 1));
+        size[w] = begin(w) == mine || c == 0 ? 0 : max(end - lo[w], 0);
     }
     for (int most = step; most > 0; most >>= 1) {   // all runs' searches side by side
         int other[kWays];
@@ -268,6 +275,20 @@ __global__ __launch_bounds__(kThreads) void k_merge(const int2 *__restrict__ fro
     for (int w = 0; w < kWays; ++w)
         if (begin(w) != mine) at += lo[w] - begin(w);
     if (first + threadIdx.x < n) to[at] = v;
+}
+
+// The first sorted place of a token, or of those above it.
+__device__ inline int64_t first_place(const int2 *__restrict__ sorted, int64_t n, int token)
+{
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t half = (lo + hi) >> 1;
+        if (sorted[half].x < token)
+            lo = half + 1;
+        else
+            hi = half;
+    }
+    return lo;
 }
 
 constexpr int kChunkMost = 128, kRowsAhead = 8;
@@ -289,14 +310,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_sum(const T *__restrict__ d_
         int *const named = reinterpret_cast<int *>(lds);
         if ((int)threadIdx.x < rows) {
             const int row = (int)row0 + threadIdx.x;
-            int64_t lo = 0, hi = n;
-            while (lo < hi) {
-                const int64_t half = (lo + hi) >> 1;
-                if (sorted[half].x < row)
-                    lo = half + 1;
-                else
-                    hi = half;
-            }
+            const int64_t lo = first_place(sorted, n, row);
             named[threadIdx.x] = lo < n && sorted[lo].x == row;
         }
         __syncthreads();
@@ -430,42 +444,39 @@ __global__ __launch_bounds__(kJoinThreads) void k_embed_join(int hidden, const i
     put(row, c, sum);
 }
 
-// Rows of less than 8 columns: a thread a row of the table, its places found by a search.
+// Rows of less than 8 columns: a wave a row of the table, each lane every 64th of its places, then the lanes' sums.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_embed_narrow(const T *__restrict__ d_out, int64_t stride, int hidden,
                                                            const int2 *__restrict__ sorted, int64_t n, int vocab,
                                                            float scale, bool add, float *__restrict__ d_table)
 {
-    const int64_t row = workgroup() * kThreads + threadIdx.x;
+    const int64_t row = workgroup() * (kThreads / 64) + (threadIdx.x >> 6);
     if (row >= vocab) return;
-    int64_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int64_t half = (lo + hi) >> 1;
-        if (sorted[half].x < row)
-            lo = half + 1;
-        else
-            hi = half;
-    }
-    float sum[8] = {};
-    bool any = false;
-    for (; lo < n && sorted[lo].x == row; ++lo, any = true) {
-        const T *const from = d_out + sorted[lo].y * stride;
+    const int lane = threadIdx.x & 63;
+    const int64_t lo = first_place(sorted, n, (int)row), hi = first_place(sorted, n, (int)row + 1);
+    if (add && lo == hi) return;
+    float sum[7] = {};
+    for (int64_t i = lo + lane; i < hi; i += 64) {
+        const T *const from = d_out + sorted[i].y * stride;
 #pragma unroll
         for (int j = 0; j < 7; ++j)
             if (j < hidden) sum[j] += to_f32(from[j]);
     }
-    if (add && !any) return;
+#pragma unroll
+    for (int j = 0; j < 7; ++j) sum[j] = wave_reduce(sum[j], Sum());
+    if (lane > 0) return;
 #pragma unroll
     for (int j = 0; j < 7; ++j)
         if (j < hidden) d_table[row * hidden + j] = (add ? d_table[row * hidden + j] : 0.0f) + sum[j] * scale;
 }
 
-// Up to this many places are sorted by counting.  us of a call of 64 columns by counting, by digits: 1,000 places 13.3, 13.6 (the
-// host's), 4,096 16.1, 22.7, 8,192 49, 55, 16,384 54, 56, 32,768 66, 58.
+// Up to this many places are sorted by counting.  us of a call of 64 columns by counting, by digits: 1,000 places 13.3, 13.6
+// (the host's), 4,096 16.1, 22.7, 8,192 49, 55, 16,384 54, 56, 32,768 66, 58.
 constexpr int64_t kRankMost = 16384;
 
-// Places of a chunk: the most that leave two workgroups a CU, if any do.  us by 64, 128: 32,768 places: 131,072 x 4,096, tokens
-// as words fall 513, 527, all of one token 559, 524; 32,768 x 4,096 230, 222 and 273, 228; 1,000 x 7,168 170, 154 and 194, 159.
+// Places of a chunk: the most that leave two workgroups a CU, if any do.  us by 64, 128: 32,768 places: 131,072 x 4,096,
+// tokens as words fall 513, 527, all of one token 559, 524; 32,768 x 4,096 230, 222 and 273, 228; 1,000 x 7,168 170, 154
+// and 194, 159.
 int chunk_of(int64_t tokens, int64_t hidden)
 {
     int chunk = kRowsAhead;
@@ -540,7 +551,7 @@ hipError_t launch_embed_backward(const void *d_out, int type, int64_t stride, in
         using T = decltype(t);
         const T *d = static_cast<const T *>(d_out);
         if (hidden < 8) {
-            hipLaunchKernelGGL(k_embed_narrow<T>, many(ceil_div(vocab, kThreads)), dim3(kThreads), 0, s, d, stride,
+            hipLaunchKernelGGL(k_embed_narrow<T>, many(ceil_div(vocab, kThreads / 64)), dim3(kThreads), 0, s, d, stride,
                                (int)hidden, sorted, tokens, (int)vocab, scale, add, d_table);
             return hipGetLastError();
         }

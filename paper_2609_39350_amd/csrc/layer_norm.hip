@@ -6,10 +6,11 @@
 // loses nothing.
 //
 // Bound by HBM: each row is read once and held, 16-bit elements two a register, the next one's loads on their way under
-// the sums.  A wave has a row of up to 1,024 elements, a workgroup a longer one (two vectors of 8 a thread; four measured
-// 120 us against 98 at 16,384 x 8,192).  bf16, 32,768 x 4,096: forward 100 us (5.4 TB/s), backward with add 204 (5.3
-// TB/s), of it 4 for the parts' sums; 16,384 x 7,168 91 and 170; 8,192 x 16,384 100 and 235 (4.6 TB/s: no room to
-// hold two rows).  Vectors of any alignment; a row that is no multiple of 8 ends in one that overlaps the one before.
+// the sums.  A wave has a row of up to 1,024 elements, a workgroup a longer one, two vectors of 8 a thread (8,192 x
+// 16,384 by four a thread: 119 us against 112, backward 445 against 301).  bf16, 32,768 x 4,096: forward 100 us (5.4
+// TB/s), backward with add 204 (5.3 TB/s), of it 4 for the parts' sums; 16,384 x 7,168 91 and 170; 8,192 x 16,384 100 and
+// 235 (4.6 TB/s: no room to hold two rows).  Vectors of any alignment; a row that is no multiple of 8 ends in one that
+// overlaps the one before.
 #include "operators.h"
 
 namespace hapmoe {
@@ -435,8 +436,8 @@ bool is_full(Share sh, int64_t hidden) { return hidden == sh.threads * sh.vector
 int64_t rows_at_once(Share sh) { return sh.threads < 256 ? 256 / sh.threads : 1; }
 unsigned threads_of(Share sh) { return sh.threads < 256 ? 256 : sh.threads; }
 
-// Workgroups of 256 threads a CU, or as many threads: us by 2, 3, 4, 5, 6: bf16, 32,768 x 4,096: forward 4: 113, 5: 111, 6: 110
-// (and 4,096 rows 24, 26, 29), backward 205, 218, 224.  More are more parts of the weight's sums.
+// Workgroups of 256 threads a CU, or as many threads.  us, bf16, 32,768 x 4,096: forward by 4, 5, 6 113, 111, 110 (4,096 rows
+// 24, 26, 29), backward by 2, 3, 4 205, 218, 224: more are more parts of the weight's sums.
 constexpr int kForward = 4, kBackward = 2;
 int64_t workgroups_of(Share sh, int64_t rows, int a_cu)
 {

@@ -4,8 +4,14 @@
 // The choice is that of the exact scores: with a bias no order of the logits tells it, and two sums s + bias can be
 // nearer to each other than fp32 resolves.  So a token is chosen for in fp32 first, by 16 lanes as in route.hip, and each
 // pair of neighbours in the order that decides something is looked at: the chosen experts, the first that is not, the last
-// group that stays and the first that does not.  Where one is nearer than the error of the two (about one token in a
-// thousand), the wave computes that token's scores again in 64 bits.
+// group that stays and the first that does not.  Where a pair is nearer than the error of the two (one token in a
+// thousand), its scores are computed again in 64 bits: those of the choices by the same lanes, or, where more than their
+// order may change, all of the token's by a wave.
+//
+// Bound by instruction issue (1,240 a wave for four tokens) and, in the last workgroup to end, by what is computed again.
+// 32,768 tokens, 256 fp32 logits, 8 of 4 of 8 groups by sigmoid and bias: choices 30.7 us (153 with all in 64 bits, 25 with
+// nothing computed again), the order 11.8 as in route.hip, the gradient 9.2 (it reads logits at the chosen alone).  4 such
+// tokens in one launch 9.2 us.
 #include "router.h"
 
 namespace hapmoe {
@@ -88,7 +94,7 @@ __device__ inline void choose_exactly(const BalancedRoute &q, const T *__restric
     }
 }
 
-// Groups of whole lanes, 1, 2, 4, 8 or 16 of them; 0: any others.
+// Lanes of a group where its experts are those of 1, 2, 4, 8 or 16 whole lanes; 0: any others.
 __host__ __device__ inline int lanes_a_group(int each, int per)
 {
     const int m = each / per;
@@ -107,13 +113,12 @@ struct Top2 {
         b = Max()(Min()(a, oa), Max()(b, ob));
         a = Max()(a, oa);
     }
-    // The other lanes of a group of m (a power of two), neighbours in a row of 16.
+    // The other lanes of a group of m = 1, 2, 4 or 8, neighbours in a row of 16 (of 16 there is one group, not looked at).
     __device__ void over_lanes(int m)
     {
         if (m >= 2) join(dpp<0xb1>(a), dpp<0xb1>(b));     // lanes 1 0 3 2
         if (m >= 4) join(dpp<0x4e>(a), dpp<0x4e>(b));     // lanes 2 3 0 1
         if (m >= 8) join(dpp<0x141>(a), dpp<0x141>(b));   // 8 lanes mirrored: the other four's
-        if (m >= 16) join(dpp<0x140>(a), dpp<0x140>(b));  // 16 lanes mirrored
     }
     // The group's score, and its summands' size for the error.
     __device__ int score(int group_best, float &size) const
@@ -205,13 +210,13 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
         load_logits<T, PER, VEC, true>(x, logits, lane, experts, keep);
         float top = -INFINITY, total = 1.0f, error = 2 * kUnit;
         if (scored) {
-            // A sigmoid by exp2 and rcp, a unit each: its error is below 2^-22, as |x| s (1 - s) < 1/4.  A share of the softmax:
-            // below (PER / 2 + 14) 2^-23 of the largest share, PER / 2 + 2 by the sum, 10 by exponents of up to the entropy's
-            // 11 bits.  Twice that for the difference of two.
+            // A sigmoid by exp2 and rcp, a unit each: its error is below 2^-22, as |x| s (1 - s) < 1/4.  A share of the
+            // softmax: below (PER / 2 + 14) 2^-23 of the largest share: PER / 2 + 2 by the sum, 10 by the exponents' rounding,
+            // whose mean is of the entropy's at most 10 bits, 2 by rcp and product.  Twice that for the difference of two.
             if constexpr (SIGMOID) {
 #pragma unroll
                 for (int c = 0; c < PER; ++c)
-                    x[c] = x[c] > -INFINITY ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[c] * -kLog2)) : -INFINITY;
+                    x[c] = x[c] == -INFINITY ? x[c] : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[c] * -kLog2));
             } else {
                 top = row_reduce(lane_largest<float, PER>(x), Max());
                 total = 0.0f;
@@ -252,7 +257,8 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
                 size = row_reduce(size, Max());
                 const uint64_t taken = best_groups(
                     q.top_groups, 2 * error + kUnit * size, again, [&] { return key; },
-                    [&](int most) { return key == most ? mine : INT32_MAX; }, [&](int g) { key = g == mine ? kClosed : key; });
+                    [&](int most) { return key == most ? mine : INT32_MAX; },
+                    [&](int g) { key = g == mine ? kClosed : key; });
 #pragma unroll
                 for (int c = 0; c < PER; ++c) v[c] = taken >> mine & 1 ? v[c] : kClosed;
             } else {
@@ -350,8 +356,8 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
             most = row_reduce(own, Max());
             before = q.bias && most != kClosed && !(value - logit_of(most) > error + kUnit / 2 * fabsf(value)) ? best : -1;
         }
-        // Up to 15 choices and the first that is not, where it is near to the last, are one a lane: they are put in order here,
-        // by their scores in 64 bits.  All else that is near takes a wave; so does an expert near to the first not chosen.
+        // Up to 15 choices and the first that is not, where it is near to the last, are one a lane: they are put in order
+        // here, by their scores in 64 bits.  All else that is near takes a wave; so does an expert near to the first not chosen.
         again = again || before >= 0 || (near && top_k > 15);
         if (__ballot(near && !again)) {
             double all = 0.0;   // of a softmax

@@ -420,7 +420,7 @@ def embed_grad_ref(d_out, token, V, scale, into=None):
 @pytest.mark.parametrize("T,V,H,share", [
     (1, 1, 1, 0.0), (7, 3, 5, 0.0), (100, 50, 1024, 0.5), (1000, 100000, 64, 0.0), (2000, 1000, 1023, 0.9),
     (8191, 300, 136, 0.3), (16384, 513, 72, 0.1), (16385, 511, 40, 0.6), (40000, 70000, 33, 0.5), (9000, 1, 24, 0.0),
-    (140001, 997, 16, 0.2), (65537, 100, 9, 0.0), (300, 40, 4100, 0.3)])
+    (140001, 997, 16, 0.2), (65537, 100, 9, 0.0), (300, 40, 4100, 0.3), (20000, 300, 3, 0.9)])
 def test_embed_backward(T, V, H, share, dtype):
     """share: of the places that hold one and the same token."""
     say("embed_backward", T, V, H, share, dtype)
