@@ -392,22 +392,31 @@ __global__ __launch_bounds__(kJoinThreads) void k_embed_join(int hidden, const i
     const int64_t which = workgroup() * (kThreads / lanes) + thread / lanes, lo = which * chunk, hi = lo + chunk;
     const Columns c(hidden, blockIdx.y * lanes + thread % lanes);
     int token = vocab;
-    if (hi < n && c.skip < 8) {
+    if (hi < n) {
         token = sorted[hi - 1].x;
         if (sorted[hi].x != token || (lo > 0 && sorted[lo - 1].x == token)) token = vocab;
     }
-    const bool has = token != vocab;
-    if (!__syncthreads_or(has)) return;
-    int64_t chunks = 0;   // behind this one that begin with the token
-    if (has)
-        for (int64_t a = 0, b = (n - hi + chunk - 1) / chunk; a < b;) {
-            const int64_t half = (a + b) >> 1;
-            if (sorted[hi + half * chunk].x == token)
-                a = half + 1;
-            else
-                b = half;
-            chunks = a;
+    const bool goes_on = token != vocab, has = goes_on && c.skip < 8;
+    if (!__syncthreads_or(goes_on)) return;
+    // chunks behind this one that begin with the token, of `size` that may: by 64 of them at once where a wave has one token
+    // (in all its lanes, those without columns too)
+    int64_t chunks = 0, size = goes_on ? (n - hi + chunk - 1) / chunk : 0;
+    if (lanes >= 64) {
+        while (size > 0) {
+            const int64_t step = (size + 63) / 64, at = ((threadIdx.x & 63) + 1) * step - 1;
+            const bool more = at < size && sorted[hi + (chunks + at) * chunk].x == token;
+            const int64_t passed = (int64_t)__popcll(__ballot(more)) * step;
+            chunks += passed;
+            size = min(step - 1, size - passed);
         }
+    } else {
+        while (size > 0) {
+            const int64_t half = size >> 1;
+            const bool more = sorted[hi + (chunks + half) * chunk].x == token;
+            chunks += more ? half + 1 : 0;
+            size = more ? size - half - 1 : half;
+        }
+    }
     // sum 0 is this chunk's, sum i of the chunk i behind it
     const int64_t each = (chunks + kQuarters) / kQuarters, first = min(quarter * each, chunks + 1);
     const int64_t last = min(first + each, chunks + 1);
