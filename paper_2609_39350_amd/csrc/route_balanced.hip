@@ -183,8 +183,8 @@ constexpr int kAgain = -2;   // in place of a token's first choice: it is chosen
 
 // LDS: [here * top_k] choices, then the tokens' keys and, where groups are not whole lanes, their scores; when those are
 // done the counts of the order.
-template <typename T, int PER, bool VEC, bool ALONE, bool SIGMOID>
-__global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(BalancedRoute q, int group, int bits)
+template <typename T, int PER, bool VEC, bool SIGMOID>
+__global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(BalancedRoute q, int group, int bits, bool alone)
 {
     constexpr int kChoose = choose_threads(PER), kWaves = kChoose / 64;
     constexpr float kUnit = 1.0f / (1 << 22), kLog2 = 1.44269504f;
@@ -433,8 +433,13 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
     __syncthreads();
     for (int e = threadIdx.x; e < kWaves * experts; e += kChoose) sums[e] = 0;
     __syncthreads();
-    order_rows<kChoose, ALONE>(chosen, sums, sh, here, top_k, first, experts, bits, q.place, static_cast<int32_t *>(q.ws),
-                               q.count, q.offset, q.slot);
+    int32_t *const hist = static_cast<int32_t *>(q.ws);
+    if (alone)
+        order_rows<kChoose, true>(chosen, sums, sh, here, top_k, first, experts, bits, q.place, hist, q.count, q.offset,
+                                  q.slot);
+    else
+        order_rows<kChoose, false>(chosen, sums, sh, here, top_k, first, experts, bits, q.place, hist, q.count, q.offset,
+                                   q.slot);
 }
 
 }  // namespace
@@ -459,11 +464,10 @@ hipError_t launch_route_balanced(const BalancedRoute &a, hipStream_t s)
             const size_t lds = (((rows_here + 3) & ~3) + (keys + scores > sums ? keys + scores : sums)) * sizeof(int);
             auto kernel = [&](auto sigmoid) {
                 constexpr bool S = decltype(sigmoid)::value;
-                return alone ? (vec ? k_choose_balanced<T, PER, true, true, S> : k_choose_balanced<T, PER, false, true, S>)
-                             : (vec ? k_choose_balanced<T, PER, true, false, S> : k_choose_balanced<T, PER, false, false, S>);
+                return vec ? k_choose_balanced<T, PER, true, S> : k_choose_balanced<T, PER, false, S>;
             };
             hipLaunchKernelGGL((a.sigmoid ? kernel(std::true_type()) : kernel(std::false_type())), many(workgroups),
-                               dim3(kChoose), lds, s, a, group, bits);
+                               dim3(kChoose), lds, s, a, group, bits, alone);
             return hipGetLastError();
         });
     });
