@@ -11,8 +11,8 @@
 //
 // Bound by HBM where the table's gradient is written whole, by launches that wait for each other where few rows are added
 // to.  bf16, 32,768 places, tokens as words fall, of 131,072 x 4,096: forward 77 us (0.38 GB, 5.0 TB/s), sort 12, segments
-// together 14, sums and clears 455 (2.4 GB, 5.3 TB/s; a fill of as much takes 5.4 to 6.8), what goes on 14.  4,001
-// places of 1,023 fp16 added to: 4.8 forward, then 5.3, 8.0 and 7.6.
+// together 12, sums and clears 455 (2.4 GB, 5.3 TB/s; a fill alone reaches 5.4 to 6.8), what goes on 12.  4,001
+// places of 1,023 fp16 added to: 4.8 forward, then 5.4, 8.1 and 6.4.
 #include "operators.h"
 
 namespace hapmoe {
