@@ -130,27 +130,19 @@ struct Top2 {
     }
 };
 
-// Of a row of 16 lanes the groups that stay.  largest(): a lane's best score; find(most): the lowest group that a lane has
-// it for; close(g).  near: whether the last of them and the first that goes are within `error` of each other.
-template <typename L, typename F, typename C>
-__device__ inline uint64_t best_groups(int top_groups, float error, bool &near, L largest, F find, C close)
+// Of a row of 16 lanes, whose groups are m lanes each and have their scores' keys in the first of them (`first`, kClosed
+// in the others): how many groups go before the lane's, those of a larger key and lower ones of the same.  Fifteen looks
+// that do not wait for each other, where taking the best of those left does (2,400 cycles for 4 of 8).
+template <int R = 1>
+__device__ inline int groups_before(int first, int key, int lane, int m)
 {
-    uint64_t taken = 0;
-    float last = 0.0f;
-    for (int j = 0;; ++j) {
-        const int most = row_reduce(largest(), Max());
-        if (most == kClosed) break;
-        const float value = logit_of(most);
-        if (j == top_groups) {
-            near = !(last - value > error);
-            break;
-        }
-        const int g = row_reduce(find(most), Min());
-        taken |= 1ull << g;
-        close(g);
-        last = value;
-    }
-    return taken;
+    const int other = dpp<0x120 + R>(first);   // of lane - R, round the row
+    const bool lower = ((lane - R) & 15) < (lane & -m);
+    const int before = other > key || (other == key && lower) ? 1 : 0;
+    if constexpr (R < 15)
+        return before + groups_before<R + 1>(first, key, lane, m);
+    else
+        return before;
 }
 
 // Weights from the logit z of a lane's choice or choices (-inf: none), N a lane; reduce: over the token's lanes.
@@ -210,6 +202,13 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
         load_logits<T, PER, VEC, true>(x, logits, lane, experts, keep);
         float top = -INFINITY, total = 1.0f, error = 2 * kUnit;
         if (scored) {
+            float bias[PER] = {};
+            if (q.bias) {
+                int at = lane * PER;
+                asm volatile("" : "+v"(at));   // loaded for every token: held they are as many registers as the keys
+#pragma unroll
+                for (int c = 0; c < PER; ++c) bias[c] = q.bias[VEC ? at + c : min(at + c, experts - 1)];
+            }
             // A sigmoid by exp2 and rcp, a unit each: its error is below 2^-22, as |x| s (1 - s) < 1/4.  A share of the
             // softmax: below (PER / 2 + 14) 2^-23 of the largest share: PER / 2 + 2 by the sum, 10 by the exponents' rounding,
             // whose mean is of the entropy's at most 10 bits, 2 by rcp and product.  Twice that for the difference of two.
@@ -232,12 +231,8 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
 #pragma unroll
                 for (int c = 0; c < PER; ++c) x[c] *= size;
             }
-            if (q.bias) {
-                int at = lane * PER;
-                asm volatile("" : "+v"(at));   // loaded for every token: held they are as many registers as the keys
 #pragma unroll
-                for (int c = 0; c < PER; ++c) x[c] += q.bias[VEC ? at + c : min(at + c, experts - 1)];
-            }
+            for (int c = 0; c < PER; ++c) x[c] += bias[c];
 #pragma unroll
             for (int c = 0; c < PER; ++c) v[c] = x[c] > -INFINITY ? key_of(x[c]) : kClosed;   // a NaN bias closes too
         } else {
@@ -252,15 +247,14 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
 #pragma unroll
                 for (int c = 1; c < PER; ++c) best.take(v[c]);
                 best.over_lanes(m);
-                int key = best.score(q.group_best, size);
-                const int mine = lane / m;
+                const int key = best.score(q.group_best, size);
                 size = row_reduce(size, Max());
-                const uint64_t taken = best_groups(
-                    q.top_groups, 2 * error + kUnit * size, again, [&] { return key; },
-                    [&](int most) { return key == most ? mine : INT32_MAX; },
-                    [&](int g) { key = g == mine ? kClosed : key; });
+                const int better = groups_before(lane % m == 0 ? key : kClosed, key, lane, m);   // by all lanes
+                const bool stays = key != kClosed && better < q.top_groups;
+                const int last = row_reduce(stays ? key : INT32_MAX, Min()), next = row_reduce(stays ? kClosed : key, Max());
+                again = next != kClosed && !(logit_of(last) - logit_of(next) > 2 * error + kUnit * size);
 #pragma unroll
-                for (int c = 0; c < PER; ++c) v[c] = taken >> mine & 1 ? v[c] : kClosed;
+                for (int c = 0; c < PER; ++c) v[c] = stays ? v[c] : kClosed;
             } else {
                 int *const score = sums + kChoose / 16 * key_row(PER) + (threadIdx.x >> 4) * HAPMOE_MAX_GROUPS;
                 wave_order();
@@ -276,23 +270,25 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
                     score[g] = best.score(q.group_best, size);
                 }
                 size = row_reduce(size, Max());
-                const uint64_t taken = best_groups(
-                    q.top_groups, 2 * error + kUnit * size, again,
-                    [&] {
-                        int own = kClosed;
+                uint64_t taken = 0;
+                float last = 0.0f;
 #pragma unroll 1
-                        for (int g = lane; g < q.groups; g += 16) own = Max()(own, score[g]);
-                        return own;
-                    },
-                    [&](int most) {
-                        int g = lane;
-#pragma unroll 1
-                        while (g < q.groups && score[g] != most) g += 16;
-                        return g < q.groups ? g : INT32_MAX;
-                    },
-                    [&](int g) {
-                        if (g % 16 == lane) score[g] = kClosed;
-                    });
+                for (int j = 0;; ++j) {   // the best of those left, the lowest of equal ones
+                    int most = kClosed;
+                    for (int g = lane; g < q.groups; g += 16) most = Max()(most, score[g]);
+                    most = row_reduce(most, Max());
+                    if (most == kClosed) break;
+                    if (j == q.top_groups) {
+                        again = !(last - logit_of(most) > 2 * error + kUnit * size);
+                        break;
+                    }
+                    int best = lane;
+                    while (best < q.groups && score[best] != most) best += 16;
+                    best = row_reduce(best < q.groups ? best : INT32_MAX, Min());
+                    taken |= 1ull << best;
+                    if (best % 16 == lane) score[best] = kClosed;
+                    last = logit_of(most);
+                }
                 int g = lane * PER / each;
                 asm volatile("" : "+v"(g));   // the groups of PER experts again for every token, not in registers
                 int in = lane * PER - g * each;
@@ -316,15 +312,14 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
             wave_order();
         }
         int own = lane_largest<int, PER>(v), most = row_reduce(own, Max());
-        int who[2] = {-1, -1};   // choices lane and lane + 16
-        int before = -1;         // the choice before, where this one is near to it
-        for (int j = 0; j <= top_k && most != kClosed && (j < top_k || before >= 0); ++j) {
+        auto take = [&]() {   // the expert that has `most`, the lowest; `most` of those left
             int best;
             if constexpr (keys_in_lds(PER)) {
                 const int from = first_of_row(own == most);
                 int k[PER / 16], at = 0;
 #pragma unroll
                 for (int i = 0; i < PER / 16; ++i) k[i] = row[from * PER + 16 * i + lane];
+                const int others = row_reduce(lane == from ? kClosed : own, Max());   // while those are on their way
 #pragma unroll
                 for (int i = PER / 16 - 1; i >= 0; --i) {
                     const int l = first_of_row(k[i] == most);
@@ -337,6 +332,7 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
                 wave_order();
                 const int left = row_reduce(lane_largest<int, PER / 16>(k), Max());
                 own = lane == from ? left : own;
+                most = Max()(left, others);
             } else {
                 int at = PER;
 #pragma unroll
@@ -346,19 +342,54 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
 #pragma unroll
                 for (int c = 0; c < PER; ++c) v[c] = c == mine ? kClosed : v[c];
                 own = lane_largest<int, PER>(v);
+                most = row_reduce(own, Max());
             }
-            // equal logits and biases have equal sums, however near; others may not be in this order
-            if (before >= 0)
-                near = near || to_f32(logits[before]) != to_f32(logits[best]) || q.bias[before] != q.bias[best];
+            return best;
+        };
+        int who[2] = {-1, -1}, won[2] = {kClosed, kClosed};   // choices lane and lane + 16 and their keys
+        for (int j = 0; j < top_k; ++j) {
+            const int key = most, best = take();
 #pragma unroll
-            for (int h = 0; h < 2; ++h) who[h] = lane + 16 * h == j ? best : who[h];
-            const float value = logit_of(most);
-            most = row_reduce(own, Max());
-            before = q.bias && most != kClosed && !(value - logit_of(most) > error + kUnit / 2 * fabsf(value)) ? best : -1;
+            for (int h = 0; h < 2; ++h) {
+                won[h] = lane + 16 * h == j ? key : won[h];
+                who[h] = lane + 16 * h == j && key != kClosed ? best : who[h];
+            }
         }
-        // Up to 15 choices and the first that is not, where it is near to the last, are one a lane: they are put in order
-        // here, by their scores in 64 bits.  All else that is near takes a wave; so does an expert near to the first not chosen.
-        again = again || before >= 0 || (near && top_k > 15);
+        if (q.bias) {
+            // a choice and the one after it, of the next lane; the last one and the first that is not chosen
+            auto after = [&](int a, int b, int beyond, int h) {
+                const int x0 = dpp<0x12f>(a), x1 = dpp<0x12f>(b);
+                return lane + 16 * h == top_k - 1 ? beyond : h == 0 && lane < 15 ? x0 : x1;
+            };
+            auto within = [&](int key, int next) {
+                const float value = logit_of(key);
+                return key != kClosed && next != kClosed && !(value - logit_of(next) > error + kUnit / 2 * fabsf(value));
+            };
+            bool close[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) close[h] = within(won[h], after(won[0], won[1], most, h));
+            if (__ballot(close[0] || close[1])) {
+                // equal logits and biases have equal sums, however near; others may not be in this order
+                const int key = most, best = take(), extra = key != kClosed ? best : -1;
+                int found = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int next = after(who[0], who[1], extra, h);
+                    if (close[h]) {
+                        found |= to_f32(logits[who[h]]) != to_f32(logits[next]) || q.bias[who[h]] != q.bias[next] ? 1 : 0;
+                        // the first that is not chosen is near to the last, and another to it
+                        found |= lane + 16 * h == top_k - 1 && within(key, most) ? 2 : 0;
+                    }
+                }
+                found = row_reduce(found & 1, Max()) | row_reduce(found & 2, Max());
+                near = found & 1;
+                again = again || found & 2;
+                who[0] = lane == top_k ? extra : who[0];
+            }
+        }
+        // Up to 15 choices and the first that is not are one a lane: where some are near they are put in order here, by their
+        // scores in 64 bits.  All else that is near takes a wave.
+        again = again || (near && top_k > 15);
         if (__ballot(near && !again)) {
             double all = 0.0;   // of a softmax
             if constexpr (!SIGMOID) {

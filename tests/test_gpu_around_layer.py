@@ -127,6 +127,26 @@ def test_route_balanced_sums_nearer_than_fp32(T, E, k, G, TG, scores):
     check_balanced(ops.route_balanced(logits, k, **how), ref, E)
 
 
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("T,E,k,G,TG", [(500, 16, 3, 4, 2), (500, 256, 8, 8, 4), (300, 60, 4, 6, 2), (200, 512, 8, 16, 3)])
+def test_route_balanced_sums_below_zero_and_closed_groups(T, E, k, G, TG, scores):
+    """Biases that leave every sum below zero, groups closed to a token, lanes without experts beside those with."""
+    logits = normal(1, T, E)
+    logits.view(T, G, E // G)[torch.rand((T, G), generator=gen(2), device="cuda") < 0.3] = -inf
+    how = {"bias": normal(3, E) * 0.3 - 4, "scores": scores, "groups": G, "top_groups": TG}
+    check_balanced(ops.route_balanced(logits, k, **how), balanced_ref(logits, k, **how), E)
+
+
+@pytest.mark.parametrize("m", [1, 2, 4, 8])
+def test_route_balanced_equal_groups(m):
+    """Groups of one to eight lanes whose scores are the same: the lowest stay."""
+    E, G = 64, 16 // m
+    logits = normal(5, 1, E // G).repeat(70, G)
+    for TG in range(1, G + 1):
+        how = {"bias": normal(6, E // G).repeat(G) * 0.1, "groups": G, "top_groups": TG}
+        check_balanced(ops.route_balanced(logits, 4, **how), balanced_ref(logits, 4, **how), E)
+
+
 @pytest.mark.parametrize("renormalize", [False, True])
 @pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
 @pytest.mark.parametrize("G,TG", [(1, 1), (3, 2), (6, 1)])
