@@ -8,10 +8,10 @@
 // thousand), its scores are computed again in 64 bits: those of the choices by the same lanes, or, where more than their
 // order may change, all of the token's by a wave.
 //
-// Bound by instruction issue (1,240 a wave for four tokens) and, in the last workgroup to end, by what is computed again.
-// 32,768 tokens, 256 fp32 logits, 8 of 4 of 8 groups by sigmoid and bias: choices 30.7 us (153 with all in 64 bits, about 25
-// with nothing computed again), the order 11.8 as in route.hip, the gradient 9.5 (it reads logits at the chosen alone).  4
-// such tokens in one launch 9.2 us, 14.5 where one is computed again by a wave.
+// Bound by instruction issue (1,390 a wave for four tokens, 79 % of the time) and, in the last workgroup to end, by what is
+// computed again.  32,768 tokens, 256 fp32 logits, 8 of 4 of 8 groups by sigmoid and bias: choices 28.7 us (153 with all in
+// 64 bits), the order 11.6 as in route.hip, the gradient 9.0 (it reads logits at the chosen alone).  4 such tokens in one
+// launch 7.9 us, five more where one is computed again by a wave.
 #include "router.h"
 
 namespace hapmoe {
