@@ -120,13 +120,14 @@ struct Top2 {
         if (m >= 4) join(dpp<0x4e>(a), dpp<0x4e>(b));     // lanes 2 3 0 1
         if (m >= 8) join(dpp<0x141>(a), dpp<0x141>(b));   // 8 lanes mirrored: the other four's
     }
-    // The group's score, and its summands' size for the error.
+    // The group's score, and its summands' size for the error.  A group with an open expert is open: a sum past fp32's ends
+    // is the end, not an infinity, and its size, which is one, has the group's place found in 64 bits.
     __device__ int score(int group_best, float &size) const
     {
         if (a == kClosed) return kClosed;
         const float x = logit_of(a), y = group_best > 1 && b != kClosed ? logit_of(b) : 0.0f;
         size = fmaxf(size, fabsf(x) + fabsf(y));
-        return key_of(x + y);
+        return key_of(fminf(fmaxf(x + y, -__FLT_MAX__), __FLT_MAX__));
     }
 };
 
