@@ -29,7 +29,7 @@ STATE_BYTES = {32: 18, 8: 12}   # of an expert parameter on the GPU: copy, gradi
 
 def router_forward(x, router, top_k, balance=None):
     """The logits and the routing.  balance: None, or the arguments of a router whose choice is balanced: scores, bias,
-    groups, top_groups, group_best, scale (``operators.route_balanced``)."""
+    groups, top_groups, group_best, keep, renormalize, scale (``operators.route_balanced``)."""
     logits = x @ router.T
     if balance is None:
         return logits, operators.route(logits, top_k)
@@ -41,8 +41,8 @@ def router_backward(x, router, logits, routing, d_weight, balance=None):
     if balance is None:
         d_logits = operators.route_backward(logits, routing, d_weight)
     else:
-        d_logits = operators.route_balanced_backward(logits, routing, d_weight,
-                                                     **{k: balance[k] for k in ("scores", "scale") if k in balance})
+        of_weights = {k: balance[k] for k in ("scores", "keep", "renormalize", "scale") if k in balance}
+        d_logits = operators.route_balanced_backward(logits, routing, d_weight, **of_weights)
     return d_logits.T @ x, (d_logits @ router).float()
 
 
@@ -214,7 +214,7 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
     then runs by itself at its whole size (by equal parts of its experts, where they are more than it takes).  Returns
     ns of the parts for one micro-batch, forward and backward, the optimizer's ns a parameter and the router's counts.
 
-    balance: as in ``router_forward``; of a bias of all experts, those that run have the first entries.  vocab: not 0,
+    balance: as in ``router_forward``; what runs has the first entries of bias and keep.  vocab: not 0,
     the layer runs in its place (``block_step``), with an embedding of that many tokens, and the ns of embedding, norm and
     dropout come too."""
     m = problem["model"]
@@ -231,13 +231,12 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
     while experts // part * 3 * width * hidden * STATE_BYTES[state_bits] > limit_bytes and \
             experts % (2 * part) == 0 and experts // (2 * part) >= top_k and tokens % (2 * part) == 0:
         part *= 2
-    def of(n):   # the balance of the first n experts
-        if balance is None or balance.get("bias") is None:
-            return balance
-        return dict(balance, bias=balance["bias"][:n])
+    def of(n, rows):   # the balance of the first n experts and the first rows
+        cut = {"bias": n, "keep": rows}
+        return balance and {k: v[:cut[k]] if k in cut and v is not None else v for k, v in balance.items()}
 
     size = tokens // part, hidden, width, experts // part, top_k, state_bits
-    how = {"seed": seed, "balance": of(experts // part)}
+    how = {"seed": seed, "balance": of(experts // part, tokens // part)}
     run = Block(*size, vocab=vocab, **how) if vocab else Layer(*size, **how)
     got, ns = _times(run.step, warmup, steps)
     route_ns = ns["route"]
@@ -245,7 +244,7 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
         cut = 1   # where the router cannot take all experts at once
         while experts // cut > operators.MAX_EXPERTS:
             cut *= 2
-        alone = _router_step(tokens, hidden, experts // cut, top_k, seed, of(experts // cut))
+        alone = _router_step(tokens, hidden, experts // cut, top_k, seed, of(experts // cut, tokens))
         route_ns = _times(alone, warmup, steps)[1]["route"] * cut
     params = experts // part * 3 * width * hidden
     around = {f"{name}_ns": ns[name] * part for name in ("embed", "norm", "dropout") if name in ns}
