@@ -206,10 +206,24 @@ def _times(step, warmup, steps):
     return got, {name: sorted(v)[len(v) // 2] for name, v in spent.items()}
 
 
+def parts(experts, top_k, tokens, fits, balance=None):
+    """How many equal parts of the experts and the tokens: doubled until fits(experts of a part), while both are whole, the
+    groups of a balance are too and those that stay have top_k experts."""
+    groups = (balance or {}).get("groups", 1)
+    stay = (balance or {}).get("top_groups") or groups
+    n = 1
+    while not fits(experts // n) and experts % (2 * n) == 0 and tokens % (2 * n) == 0:
+        left = experts // (2 * n)
+        if left % groups or left // groups * stay < top_k:
+            break
+        n *= 2
+    return n
+
+
 def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=100 * 10**9, seed=0, balance=None, vocab=0):
     """Time the MoE layer ``layer`` (the first, if None) of a problem's model on the current device.
 
-    Where all its experts do not fit ``limit_bytes``, an equal part of them takes an equal part of the tokens and
+    Where all its experts do not fit ``limit_bytes``, an equal part of them (``parts``) takes an equal part of the tokens and
     the times of the experts and of the rows' sum count for the whole; the router, whose work is tokens times experts,
     then runs by itself at its whole size (by equal parts of its experts, where they are more than it takes).  Returns
     ns of the parts for one micro-batch, forward and backward, the optimizer's ns a parameter and the router's counts.
@@ -227,10 +241,8 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
     experts, hidden, top_k = int(m["n_experts"]), int(m["hidden"]), int(m["top_k"])
     tokens = int(m["seq_len"]) * int(m["micro_batch_size"])
     width = max(1, int(m["params_expert"][layer]) // (3 * experts * hidden))
-    part = 1
-    while experts // part * 3 * width * hidden * STATE_BYTES[state_bits] > limit_bytes and \
-            experts % (2 * part) == 0 and experts // (2 * part) >= top_k and tokens % (2 * part) == 0:
-        part *= 2
+    part = parts(experts, top_k, tokens, lambda n: n * 3 * width * hidden * STATE_BYTES[state_bits] <= limit_bytes, balance)
+
     def of(n, rows):   # the balance of the first n experts and the first rows
         cut = {"bias": n, "keep": rows}
         return balance and {k: v[:cut[k]] if k in cut and v is not None else v for k, v in balance.items()}
