@@ -87,13 +87,19 @@ def block_step(token, table, norm, router, experts, d_out, top_k, drop, grad, ma
     token [tokens], table [vocab, hidden], norm: the norm's weight and bias, drop: (p, seed, offset) of the dropout, grad
     [vocab, hidden] fp32: the table's gradient, which this step's is added to; the rest as in ``layer_step``, whose
     result comes with the block's output, the gradient of x and those of the norm."""
+    return _in_place(token, table, norm, d_out, drop, grad, mark,
+                     lambda n, d_layer: layer_step(n, router, experts, d_layer, top_k, mark, balance))
+
+
+def _in_place(token, table, norm, d_out, drop, grad, mark, layer):
+    """``block_step`` of any layer(its input, the gradient of its output), which returns output "out" and gradient "d_x"."""
     x = operators.embed(token, table)
     mark("embed")
     n, mean, rstd = operators.layer_norm(x, *norm)
     mark("norm")
     d_layer = operators.dropout_backward(d_out, *drop)
     mark("dropout")
-    got = layer_step(n, router, experts, d_layer, top_k, mark, balance)
+    got = layer(n, d_layer)
     out = operators.dropout(got["out"], *drop, residual=x)
     mark("dropout")
     d_x, d_norm, d_norm_bias = operators.layer_norm_backward(got["d_x"], x, norm[0], mean, rstd, add=d_out)
@@ -183,6 +189,16 @@ def _router_step(tokens, hidden, experts, top_k, seed, balance=None):
     return step
 
 
+def _around_step(tokens, hidden, top_k, vocab, seed):
+    """What stands around a layer of this size, forward and backward, without the layer: its output is its input."""
+    block = Block(tokens, hidden, 1, top_k, top_k, seed=seed, vocab=vocab)
+
+    def step(mark):
+        return _in_place(block.token, block.table, block.norm, block.d_out, (block.p, seed, 0), block.grad, mark,
+                         lambda n, d_layer: {"out": n, "d_x": d_layer})
+    return step
+
+
 def _times(step, warmup, steps):
     """What the last of warmup + steps calls of step(mark) returned, and the median ns of what it marks, without the
     first warmup."""
@@ -225,8 +241,9 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
 
     Where all its experts do not fit ``limit_bytes``, an equal part of them (``parts``) takes an equal part of the tokens and
     the times of the experts and of the rows' sum count for the whole; the router, whose work is tokens times experts,
-    then runs by itself at its whole size (by equal parts of its experts, where they are more than it takes).  Returns
-    ns of the parts for one micro-batch, forward and backward, the optimizer's ns a parameter and the router's counts.
+    then runs by itself at its whole size (by equal parts of its experts, where they are more than it takes), and so does
+    what stands around the layer.  Returns ns of the parts for one micro-batch, forward and backward, the optimizer's ns a
+    parameter and the router's counts.
 
     balance: as in ``router_forward``; what runs has the first entries of bias and keep.  vocab: not 0,
     the layer runs in its place (``block_step``), with an embedding of that many tokens, and the ns of embedding, norm and
@@ -259,7 +276,9 @@ def measure(problem, layer=None, steps=5, warmup=2, state_bits=32, limit_bytes=1
         alone = _router_step(tokens, hidden, experts // cut, top_k, seed, of(experts // cut, tokens))
         route_ns = _times(alone, warmup, steps)[1]["route"] * cut
     params = experts // part * 3 * width * hidden
-    around = {f"{name}_ns": ns[name] * part for name in ("embed", "norm", "dropout") if name in ns}
+    if part > 1 and vocab:
+        ns.update(_times(_around_step(tokens, hidden, top_k, vocab, seed), warmup, steps)[1])
+    around = {f"{name}_ns": ns[name] for name in ("embed", "norm", "dropout") if name in ns}
     return {**around, "layer": layer, "tokens": tokens, "hidden": hidden, "width": width, "experts": experts, "part": part,
             "route_ns": route_ns, "combine_ns": ns["combine"] * part, "experts_ns": ns["experts"] * part,
             "opt_ns_per_param": ns["optimizer"] / params,
