@@ -325,14 +325,20 @@ def main(argv=None):
     p.add_argument("--state-bits", type=int, default=32, choices=(8, 32))
     p.add_argument("--steps", type=int, default=5)
     p.add_argument("--scores", choices=sorted(operators.SCORES), help="a router whose choice is balanced, by these scores")
-    p.add_argument("--groups", type=int, default=1, help="its groups of experts")
+    p.add_argument("--groups", type=int, help="its groups of experts; none given: 1")
     p.add_argument("--top-groups", type=int, help="those that stay; none given: all")
     p.add_argument("--block", action="store_true", help="the layer with its embedding, norm and dropout")
-    p.add_argument("--vocab", type=int, default=32768, help="tokens of the embedding")
+    p.add_argument("--vocab", type=int, help="tokens of its embedding; none given: 32768")
     a = p.parse_args(argv)
+    for needs, given, names in ((a.scores, (a.groups, a.top_groups), "--groups and --top-groups: with --scores"),
+                                (a.block, (a.vocab,), "--vocab: with --block")):
+        if not needs and any(x is not None for x in given):
+            p.error(names)
+    if a.vocab is not None and a.vocab < 1:
+        p.error(f"--vocab: at least 1, not {a.vocab}")
     problem = workloads.config(a.config)
-    balance = a.scores and {"scores": a.scores, "groups": a.groups, "top_groups": a.top_groups}
-    got = measure(problem, steps=a.steps, state_bits=a.state_bits, balance=balance, vocab=a.vocab if a.block else 0)
+    balance = a.scores and {"scores": a.scores, "groups": 1 if a.groups is None else a.groups, "top_groups": a.top_groups}
+    got = measure(problem, steps=a.steps, state_bits=a.state_bits, balance=balance, vocab=(a.vocab or 32768) if a.block else 0)
     print(f"layer {got['layer']}: {got['tokens']} tokens, hidden {got['hidden']}, {got['experts']} experts of width "
           f"{got['width']}" + (f", one of {got['part']} parts run" if got["part"] > 1 else ""))
     flops = 3 * 6.0 * got["tokens"] * int(problem["model"]["top_k"]) * got["hidden"] * got["width"]
