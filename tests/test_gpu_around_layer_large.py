@@ -71,3 +71,22 @@ def test_embed(big):
     for at in range(0, ROWS, 1 << 17):
         part, mark = d_table[at:at + (1 << 17)], named[at:at + (1 << 17)]
         assert torch.equal((part != 0).any(1), mark)
+
+
+def test_layer_norm_weight_gradient(big):
+    """The sums over 2^20 rows against sums in 64 bits, taken in pieces."""
+    say("layer_norm_backward", tuple(big.shape))
+    w, b = normal(2, H), normal(3, H)
+    y, mean, rstd = ops.layer_norm(big, w, b)
+    _, d_w, d_b = ops.layer_norm_backward(y, big, w, mean, rstd)
+    sums = torch.zeros(4, H, dtype=torch.float64, device="cuda")
+    for at in range(0, ROWS, 1 << 14):
+        g, x = y[at:at + (1 << 14)].double(), big[at:at + (1 << 14)].double()
+        hat = (x - mean[at:at + (1 << 14), None].double()) * rstd[at:at + (1 << 14), None].double()
+        for n, terms in enumerate((g * hat, g)):
+            sums[2 * n] += terms.sum(0)
+            sums[2 * n + 1] += terms.abs().sum(0)
+    # additions: a workgroup's rows, of 512, a run of the parts, the runs; product and xhat
+    D = -(-ROWS // 512) + 32 + 16 + 10
+    for name, got, n in (("d_weight", d_w, 0), ("d_bias", d_b, 1)):
+        close(got, sums[2 * n], D * U32 * sums[2 * n + 1], name)
