@@ -245,6 +245,7 @@ struct Max {
     __device__ int operator()(int a, int b) const { return a > b ? a : b; }
 };
 struct Min {
+    __device__ float operator()(float a, float b) const { return fminf(a, b); }
     __device__ int operator()(int a, int b) const { return a < b ? a : b; }
 };
 struct Sum {

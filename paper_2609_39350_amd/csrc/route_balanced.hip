@@ -120,13 +120,17 @@ struct Top2 {
         if (m >= 4) join(dpp<0x4e>(a), dpp<0x4e>(b));     // lanes 2 3 0 1
         if (m >= 8) join(dpp<0x141>(a), dpp<0x141>(b));   // 8 lanes mirrored: the other four's
     }
-    // The group's score, and its summands' size for the error.  A group with an open expert is open: a sum past fp32's ends
-    // is the end, not an infinity, and its size, which is one, has the group's place found in 64 bits.
-    __device__ int score(int group_best, float &size) const
+    // The group's score, and what three roundings add to its error: of each summand, their sum and its bound, 2^-24 of the
+    // size each.  It is the group's own, so that one far off does not bring the others near.  A group with an open expert
+    // is open: a sum past fp32's ends is the end, not an infinity; its bound beyond is one, as 2^-23 of the end is more
+    // than half a step there.
+    __device__ int score(int group_best, float &rounding) const
     {
+        constexpr float kThree = 3.0f / (1 << 24);
+        rounding = 0.0f;
         if (a == kClosed) return kClosed;
         const float x = logit_of(a), y = group_best > 1 && b != kClosed ? logit_of(b) : 0.0f;
-        size = fmaxf(size, fabsf(x) + fabsf(y));
+        rounding = __builtin_fmaf(kThree, fabsf(x), kThree * fabsf(y));
         return key_of(fminf(fmaxf(x + y, -__FLT_MAX__), __FLT_MAX__));
     }
 };
@@ -242,18 +246,19 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
         }
         bool again = false, near = false;   // in the choice of groups, of experts
         if (grouped) {
-            float size = 0.0f;
+            float least = INFINITY, most_left = -INFINITY, own_error;   // of a group that stays, of one that does not
             if (m > 0) {
                 Top2 best = {v[0], kClosed};
 #pragma unroll
                 for (int c = 1; c < PER; ++c) best.take(v[c]);
                 best.over_lanes(m);
-                const int key = best.score(q.group_best, size);
-                size = row_reduce(size, Max());
+                const int key = best.score(q.group_best, own_error);
                 const int better = groups_before(lane % m == 0 ? key : kClosed, key, lane, m);   // by all lanes
                 const bool stays = key != kClosed && better < q.top_groups;
-                const int last = row_reduce(stays ? key : INT32_MAX, Min()), next = row_reduce(stays ? kClosed : key, Max());
-                again = next != kClosed && !(logit_of(last) - logit_of(next) > 2 * error + kUnit * size);
+                if (stays)
+                    least = logit_of(key) - (error + own_error);
+                else if (key != kClosed)
+                    most_left = logit_of(key) + (error + own_error);
 #pragma unroll
                 for (int c = 0; c < PER; ++c) v[c] = stays ? v[c] : kClosed;
             } else {
@@ -264,32 +269,36 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
                     *reinterpret_cast<int4 *>(row + lane * PER + c) = make_int4(v[c], v[c + 1], v[c + 2], v[c + 3]);
                 wave_order();
 #pragma unroll 1
-                for (int g = lane; g < q.groups; g += 16) {
+                for (int g0 = 0; g0 < q.groups; g0 += 16) {
+                    const int g = g0 + lane;
                     Top2 best = {kClosed, kClosed};
+                    if (g < q.groups) {
 #pragma unroll 1
-                    for (int i = 0; i < each; ++i) best.take(row[g * each + i]);
-                    score[g] = best.score(q.group_best, size);
+                        for (int i = 0; i < each; ++i) best.take(row[g * each + i]);
+                        score[g] = best.score(q.group_best, own_error);
+                    }
+                    wave_order();   // the keys in the first g0 + 16 places are read: the groups' errors go there
+                    if (g < q.groups) row[g] = __builtin_bit_cast(int, own_error);
                 }
-                size = row_reduce(size, Max());
                 uint64_t taken = 0;
-                float last = 0.0f;
 #pragma unroll 1
-                for (int j = 0;; ++j) {   // the best of those left, the lowest of equal ones
+                for (int j = 0; j < q.top_groups; ++j) {   // the best of those left, the lowest of equal ones
                     int most = kClosed;
                     for (int g = lane; g < q.groups; g += 16) most = Max()(most, score[g]);
                     most = row_reduce(most, Max());
                     if (most == kClosed) break;
-                    if (j == q.top_groups) {
-                        again = !(last - logit_of(most) > 2 * error + kUnit * size);
-                        break;
-                    }
                     int best = lane;
                     while (best < q.groups && score[best] != most) best += 16;
                     best = row_reduce(best < q.groups ? best : INT32_MAX, Min());
                     taken |= 1ull << best;
-                    if (best % 16 == lane) score[best] = kClosed;
-                    last = logit_of(most);
+                    if (best % 16 == lane) {
+                        score[best] = kClosed;
+                        least = fminf(least, logit_of(most) - (error + __builtin_bit_cast(float, row[best])));
+                    }
                 }
+                for (int g = lane; g < q.groups; g += 16)
+                    if (score[g] != kClosed)
+                        most_left = fmaxf(most_left, logit_of(score[g]) + (error + __builtin_bit_cast(float, row[g])));
                 int g = lane * PER / each;
                 asm volatile("" : "+v"(g));   // the groups of PER experts again for every token, not in registers
                 int in = lane * PER - g * each;
@@ -299,6 +308,8 @@ __global__ __launch_bounds__(choose_threads(PER)) void k_choose_balanced(Balance
                     if (++in == each) in = 0, ++g;
                 }
             }
+            least = row_reduce(least, Min()), most_left = row_reduce(most_left, Max());
+            again = most_left > -INFINITY && !(least > most_left);
         }
         if (!q.bias && scored) {   // the scores' order is that of the logits
             load_logits<T, PER, VEC, true>(x, logits, lane, experts, keep);
