@@ -116,6 +116,23 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+# A call looks at a number's class itself before it asks these, which takes 0.1 us less.
+def _whole(name, x):
+    """A whole number, of Python or of what stands for one."""
+    try:
+        return operator.index(x)
+    except Exception as e:   # a tensor of several elements has errors of its own
+        raise ValueError(f"{name}: a whole number, not {x!r}") from e
+
+
+def _real(name, x):
+    """A number that 64 bits hold."""
+    try:
+        return C.c_double(x).value
+    except Exception as e:
+        raise ValueError(f"{name}: a number, not {x!r}") from e
+
+
 def _on_device(name, t):
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
         raise ValueError(f"{name}: a tensor on the GPU")
@@ -172,6 +189,7 @@ class Routing:
 
     def __init__(self, tokens: int, experts: int, top_k: int, device="cuda"):
         need = C.c_int64(0)
+        tokens, experts, top_k = _whole("tokens", tokens), _whole("experts", experts), _whole("top_k", top_k)
         _need(0 <= tokens and 1 <= experts <= MAX_EXPERTS and 1 <= top_k <= min(experts, MAX_TOP_K)
               and tokens * top_k < 2**31, f"no routing of {tokens} tokens to {top_k} of {experts} experts")
         _check(_lib().hapmoe_route_ws_bytes(tokens, experts, top_k, C.byref(need)), "hapmoe_route_ws_bytes")
@@ -204,6 +222,7 @@ def route(logits, top_k: int, keep=None, renormalize=True, out: Routing = None) 
     (``hapmoe_route``).  keep [tokens] bool: tokens with False take none.  renormalize: weights of the
     chosen add up to 1.  out: a ``Routing`` of these sizes to write to."""
     stride = _matrix("logits", logits, _TYPES)
+    top_k = top_k if top_k.__class__ is int else _whole("top_k", top_k)
     tokens, experts = logits.shape
     if out is None:
         out = Routing(tokens, experts, top_k, logits.device)
@@ -250,6 +269,10 @@ def route_balanced(logits, top_k: int, bias=None, scores="sigmoid", groups=1, to
     tokens, experts = logits.shape
     kind = _scores(scores)
     top_groups = groups if top_groups is None else top_groups
+    if not (top_k.__class__ is groups.__class__ is top_groups.__class__ is group_best.__class__ is int):
+        top_k, groups = _whole("top_k", top_k), _whole("groups", groups)
+        top_groups, group_best = _whole("top_groups", top_groups), _whole("group_best", group_best)
+    scale = scale if scale.__class__ is float else _real("scale", scale)
     if not 1 <= groups <= MAX_GROUPS or experts % groups or not 1 <= top_groups <= groups or group_best not in (1, 2):
         raise ValueError(f"no choice of {group_best} of {top_groups} of {groups} groups of {experts} experts")
     if bias is not None:
@@ -280,6 +303,7 @@ def route_balanced_backward(logits, routing: Routing, d_weight, scores="sigmoid"
     stride = _matrix("logits", logits, _TYPES)
     tokens, experts = logits.shape
     kind = _scores(scores)
+    scale = scale if scale.__class__ is float else _real("scale", scale)
     _need((routing.tokens, routing.experts) == (tokens, experts), "routing: made for other sizes")
     k = routing.top_k
     _array("routing.expert", routing.expert, torch.int32, tokens, k)
@@ -349,6 +373,7 @@ _HALF = (torch.bfloat16, torch.float16)
 
 
 def _rows_of(x, slot, top_k):
+    top_k.__class__ is int or _whole("top_k", top_k)
     if slot is None:
         return x.shape[0]
     _array("slot", slot, torch.int32, None)
@@ -433,6 +458,7 @@ def layer_norm(x, weight, bias=None, eps=1e-5, center=True):
     rstd [rows] fp32, which ``layer_norm_backward`` takes.  center False: mean counts as 0 (root mean square norm) and
     is None.  weight and bias [hidden]: fp32 or x's type, both the same."""
     stride = _matrix("x", x, _TYPES)
+    eps = eps if eps.__class__ is float else _real("eps", eps)
     rows, hidden = x.shape
     _vector("weight", weight, (torch.float32, x.dtype), hidden)
     if bias is not None:
@@ -487,6 +513,7 @@ def embed(token, table, scale=1.0):
     """out[t] = scale * table[token[t]] for ``token`` [tokens] int32 or int64 and ``table`` [vocab, hidden]
     (``hapmoe_embed``); a token out of the table gives a row of zeros."""
     stride = _matrix("table", table, _TYPES)
+    scale = scale if scale.__class__ is float else _real("scale", scale)
     _vector("token", token, _TOKEN_BITS, None)
     vocab, hidden = table.shape
     out = table.new_empty((token.shape[0], hidden))
@@ -501,6 +528,7 @@ def embed_backward(d_out, token, vocab: int, scale=1.0, into=None):
     (``hapmoe_embed_backward``).  into: an fp32 gradient of that shape that it is added to, which is returned; rows
     without a token stay as they are.  Each row's sum has a fixed order."""
     stride = _matrix("d_out", d_out, _TYPES)
+    scale, vocab = scale if scale.__class__ is float else _real("scale", scale), _whole("vocab", vocab)
     tokens, hidden = d_out.shape
     _vector("token", token, _TOKEN_BITS, tokens)
     if not 1 <= vocab < 2**31 - 1:
@@ -526,6 +554,9 @@ def dropout(x, p, seed, offset=0, residual=None, counter=None):
     offset and the element's index alone: give every dropout of a step another offset.  counter: an int64 tensor of
     one element on the device that is added to offset when the call runs, for captured calls."""
     stride = _matrix("x", x, _TYPES)
+    p = p if p.__class__ is float else _real("p", p)
+    if not (seed.__class__ is offset.__class__ is int):
+        seed, offset = _whole("seed", seed), _whole("offset", offset)
     step = 0
     if residual is not None:
         step = _matrix("residual", residual, (x.dtype,))
@@ -593,6 +624,7 @@ class AdamW:
                 _need(copies[i].dtype in _HALF and copies[i].dtype == copies[0].dtype,
                       f"copies[{i}]: all torch.bfloat16 or all torch.float16")
                 _array(f"copies[{i}]", copies[i], copies[0].dtype, *shape)
+            decay[i] = _real(f"weight_decay[{i}]", decay[i])
             _need(decay[i] >= 0, f"weight_decay[{i}]: at least 0")
         self._index = params[0].get_device() if n else None
         self._kept = (params, m, v)
@@ -633,9 +665,16 @@ class AdamW:
                 raise ValueError(f"grads: contiguous tensors on device {index}, of one floating type of 32 or 16 bits and "
                                  "the parameters' sizes")
             a.grad_type = _TYPES[dtype]
+        if not (step.__class__ is seed.__class__ is int):
+            step, seed = _whole("step", step), _whole("seed", seed)
         if not -2**63 <= step < 2**63:   # the call's 64 bits; it refuses those below 1
             raise ValueError(f"step: {step}")
-        a.lr, a.beta1, a.beta2, a.eps, a.grad_scale, a.step = lr, beta1, beta2, eps, grad_scale, step
+        try:
+            a.lr, a.beta1, a.beta2, a.eps, a.grad_scale, a.step = lr, beta1, beta2, eps, grad_scale, step
+        except Exception:   # with the name of the one that is no number
+            for name, x in (("lr", lr), ("beta1", beta1), ("beta2", beta2), ("eps", eps), ("grad_scale", grad_scale)):
+                _real(name, x)
+            raise
         a.seed = seed & (2**64 - 1)
         if skip is not None:
             _array("skip", skip, torch.int32, 1)
