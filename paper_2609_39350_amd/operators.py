@@ -551,8 +551,8 @@ def embed_backward(d_out, token, vocab: int, scale=1.0, into=None):
 def dropout(x, p, seed, offset=0, residual=None, counter=None):
     """residual + x / (1 - p) where an element of ``x`` [rows, columns] is kept, residual (or 0) where it is dropped,
     with a chance of p rounded to a multiple of 2^-16 (``hapmoe_dropout``).  Which are dropped is a function of seed,
-    offset and the element's index alone: give every dropout of a step another offset.  counter: an int64 tensor of
-    one element on the device that is added to offset when the call runs, for captured calls."""
+    offset and the element's index alone: give every dropout of a step another offset.  counter: an int64 tensor [1] on
+    the device that is added to offset when the call runs, for captured calls."""
     stride = _matrix("x", x, _TYPES)
     p = p if p.__class__ is float else _real("p", p)
     if not (seed.__class__ is offset.__class__ is int):
@@ -644,7 +644,7 @@ class AdamW:
     def step(self, grads, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, seed=0, skip=None):
         """One step from one gradient for each parameter (contiguous, all of one type).  step: 1 for the first.
         grad_scale multiplies the gradients.  seed: of the 8-bit moments' roundings, another for every step.
-        skip: an int32 tensor of one element on the device; if it is not 0 nothing changes.
+        skip: an int32 tensor [1] on the device; if it is not 0 nothing changes.
         A captured step replays with the numbers of its capture: only with moments in 32 bits, at one lr and step."""
         n = len(self._sizes)
         if len(grads) != n:
