@@ -5,7 +5,7 @@
 // Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; 2011) of the counter (index / 8, offset) under the
 // key seed gives 128 bits, 16 for each of 8 neighbours: element i of the 8 has half i % 2 (0: the low) of word i / 2, and
 // is kept where that is at least the cut.  16 bits, because the ten rounds cost as much as moving 16 bytes does: with 32
-// for each element the rounds would bound it, not HBM: they are most of the instructions that keep the vector units 45 %
+// for each element the rounds would bound it, not HBM: they are most of the instructions that keep the vector units 50 %
 // busy.  bf16, 32,768 x 7,168: onto a residual and backward 388 us for both (2.3 GB, 6.1 TB/s).
 #include "operators.h"
 

@@ -6,13 +6,13 @@
 // tokens' order by segments of 4,096, few by counting for each place those before it, many by a stable sort of 9 bits a
 // pass in LDS; a launch puts up to 16 segments into one order, every place by a search in each of the others.  Then
 // workgroups take equal chunks of the sorted places, whatever the tokens' shares: a token that lies within a chunk is
-// written, one that goes on into the next leaves its sums in the workspace, and a last launch puts those together.  Rows without a token are cleared by
-// further workgroups of the same launch, which look for them in the sorted places.
+// written, one that goes on into the next leaves its sums in the workspace, and a last launch puts those together.  Rows
+// without a token are cleared by further workgroups of the same launch, which look for them in the sorted places.
 //
 // Bound by HBM where the table's gradient is written whole, by launches that wait for each other where few rows are added
-// to.  bf16, 32,768 places, tokens as words fall, of 131,072 x 4,096: forward 77 us (0.38 GB, 5.0 TB/s), sort 12, segments
-// together 12, sums and clears 455 (2.4 GB, 5.3 TB/s; a fill alone reaches 5.4 to 6.8), what goes on 12.  4,001
-// places of 1,023 fp16 added to: 4.8 forward, then 5.4, 8.1 and 6.4.
+// to.  bf16, 32,768 places, tokens as words fall, of 131,072 x 4,096: forward 74 to 90 us (0.38 GB, 4.2 to 5.1 TB/s), sort
+// 12, segments together 11, sums and clears 461 to 495 (2.4 GB, 4.9 to 5.2 TB/s; a fill alone reaches 5.4 to 6.8), what goes
+// on 10 to 12.  4,001 places of 1,023 fp16 added to: 4.9 forward, then 5.0, 7.7 and 6.5.
 #include "operators.h"
 
 namespace hapmoe {
@@ -380,7 +380,9 @@ __global__ __launch_bounds__(kThreads) void k_embed_sum(const T *__restrict__ d_
 }
 
 // The token that begins in a chunk and goes on: its sums there and in the chunks that follow, a run of them for each
-// quarter of the workgroup, then the quarters in their order.
+// quarter of the workgroup, then the quarters in their order.  All of a token's chunks are one workgroup's for its columns,
+// so where most places have one token and the columns are few, it is what bounds the call: 32,768 places of one token, 64
+// columns 186 us (as words fall 15), 512 83 (9), 4,096 44 (10), 7,168 28 (14).
 constexpr int kJoinThreads = 1024, kQuarters = kJoinThreads / kThreads;
 __global__ __launch_bounds__(kJoinThreads) void k_embed_join(int hidden, const int2 *__restrict__ sorted, int64_t n,
                                                              int chunk, int lanes, int vocab, float scale, bool add,
@@ -480,12 +482,13 @@ __global__ __launch_bounds__(kThreads) void k_embed_narrow(const T *__restrict__
 }
 
 // Up to this many places are sorted by counting.  us of a call of 64 columns by counting, by digits: 1,000 places 13.3, 13.6
-// (the host's), 4,096 16.1, 22.7, 8,192 49, 55, 16,384 54, 56, 32,768 66, 58.
+// (the host's), 4,096 16.1, 22.7, 8,192 49, 55, 16,384 54, 56, 32,768 66, 58.  Beyond one segment the segments are put
+// together by a launch more, 9 to 10 us: 4,096 places 5.3 to count, 4,097 5.3 and 9.1, 8,192 7.3 and 9.7, 16,384 11.9 and 9.6.
 constexpr int64_t kRankMost = 16384;
 
-// Places of a chunk: the most that leave two workgroups a CU, if any do.  us by 64, 128: 32,768 places: 131,072 x 4,096,
-// tokens as words fall 513, 527, all of one token 559, 524; 32,768 x 4,096 230, 222 and 273, 228; 1,000 x 7,168 170, 154
-// and 194, 159.
+// Places of a chunk: the most that leave two workgroups a CU, if any do, else 8.  us by 64, 128: 32,768 places: 131,072 x
+// 4,096, tokens as words fall 513, 527, all of one token 559, 524; 32,768 x 4,096 230, 222 and 273, 228; 1,000 x 7,168 170,
+// 154 and 194, 159.
 int chunk_of(int64_t tokens, int64_t hidden)
 {
     int chunk = kRowsAhead;

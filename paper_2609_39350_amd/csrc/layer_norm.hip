@@ -3,14 +3,17 @@
 //   d_x = rstd (g - mean(g) - xhat mean(g xhat)) + add,  g = d_y w,  xhat = (x - mean) rstd;  not centred: no mean(g)
 //   d_w = sum over rows of d_y xhat,  d_b = sum over rows of d_y
 // The squares are of the differences from the mean (a second look at the row, in registers), so that a row far from 0
-// loses nothing.
+// loses no more than the mean's own rounding.
 //
 // Bound by HBM: each row is read once and held, 16-bit elements two a register, the next one's loads on their way under
-// the sums.  A wave has a row of up to 1,024 elements, a workgroup a longer one, two vectors of 8 a thread (8,192 x
-// 16,384 by four a thread: 119 us against 112, backward 445 against 301).  bf16, 32,768 x 4,096: forward 100 us (5.4
-// TB/s), backward with add 204 (5.3 TB/s), of it 4 for the parts' sums; 16,384 x 7,168 91 and 170; 8,192 x 16,384 100 and
-// 235 (4.6 TB/s: no room to hold two rows).  Vectors of any alignment; a row that is no multiple of 8 ends in one that
-// overlaps the one before.
+// the sums.  A wave has a row of up to 1,024 elements, a workgroup a longer one, two vectors of 8 a thread (four a thread:
+// 8,192 x 16,384 slower by 6 % forward and half backward).  us, bf16, backward with add and the parts' sums (4 to 7):
+// 32,768 x 4,096: forward 90 to 100 (5.4 to 5.9 TB/s), backward 206 to 220 (4.9 to 5.2); 16,384 x 7,168 91 and 172 (5.4);
+// 8,192 x 16,384 99 and 236 (4.6 TB/s: no room to hold two rows).  fp32, where 128 registers do not hold a row's two
+// matrices and both sums, and 32 to 68 bytes a thread go to scratch (16-bit rows that end in part of a vector 8): 4,096 x
+// 16,384 98 and 243 (4.4 TB/s), 4,096 x 12,288 75 and 244 (3.3).  Longer rows are read two and three times, an element a
+// thread at once: bf16, 4,096 x 20,480 209 and 417.  Vectors of any alignment; a row that is no multiple of 8 ends in one
+// that overlaps the one before.
 #include "operators.h"
 
 namespace hapmoe {
@@ -442,8 +445,8 @@ bool is_full(Share sh, int64_t hidden) { return hidden == sh.threads * sh.vector
 int64_t rows_at_once(Share sh) { return sh.threads < 256 ? 256 / sh.threads : 1; }
 unsigned threads_of(Share sh) { return sh.threads < 256 ? 256 : sh.threads; }
 
-// Workgroups of 256 threads a CU, or as many threads.  us, bf16, 32,768 x 4,096: forward by 4, 5, 6 113, 111, 110 (4,096 rows
-// 24, 26, 29), backward by 2, 3, 4 205, 218, 224: more are more parts of the weight's sums.
+// Workgroups of 256 threads a CU, or as many threads.  us, bf16, 32,768 x 4,096: forward by 4, 5, 6 100, 102, 102 (4,096 rows
+// 15 by each), backward with add by 2, 3, 4 208, 218, 227 (30, 32, 35): more are more parts of the weight's sums.
 constexpr int kForward = 4, kBackward = 2;
 int64_t workgroups_of(Share sh, int64_t rows, int a_cu)
 {

@@ -4,14 +4,17 @@
 // The choice is that of the exact scores: with a bias no order of the logits tells it, and two sums s + bias can be
 // nearer to each other than fp32 resolves.  So a token is chosen for in fp32 first, by 16 lanes as in route.hip, and each
 // pair of neighbours in the order that decides something is looked at: the chosen experts, the first that is not, the last
-// group that stays and the first that does not.  Where a pair is nearer than the error of the two (one token in a
-// thousand), its scores are computed again in 64 bits: those of the choices by the same lanes, or, where more than their
-// order may change, all of the token's by a wave.
+// group that stays and the first that does not.  Where a pair is nearer than the error of the two, its scores are computed
+// again in 64 bits: those of the choices by the same lanes, or, where more than their order may change, all of the token's
+// by a wave.  Of equal inputs only a choice and its neighbour are told from near ones: groups of the same logits and
+// biases, and three that are equal over the last choice, take the wave too.
 //
-// Bound by instruction issue (1,390 a wave for four tokens, 79 % of the time) and, in the last workgroup to end, by what is
-// computed again.  32,768 tokens, 256 fp32 logits, 8 of 4 of 8 groups by sigmoid and bias: choices 28.7 us (153 with all in
-// 64 bits), the order 11.6 as in route.hip, the gradient 9.0 (it reads logits at the chosen alone).  4 such tokens in one
-// launch 7.9 us, five more where one is computed again by a wave.
+// Bound by instruction issue (1,340 a wave for four tokens, 79 % of the time) and, in the last workgroup to end, by what is
+// computed again.  32,768 tokens, 256 fp32 logits, 8 of 4 of 8 groups by sigmoid and a random bias: choices 28.3 us (153
+// with all in 64 bits), the order 11.3 as in route.hip, the gradient 9.4 (it reads logits at the chosen alone).  4 such
+// tokens in one launch 8.0 us, five more where one is computed again by a wave.  The choices with a bias of zeros: fp32
+// 30.0, bf16, which has equal logits, 35.1 (26.7 with a random bias); where a tenth of the rows are zeros 41.1 and 40.3,
+// where all are 104.
 #include "router.h"
 
 namespace hapmoe {

@@ -17,11 +17,16 @@ hipError_t launch_route_order(const int32_t *expert, int32_t *hist, int64_t grou
 namespace {
 
 // Up to this many tokens one launch: us by one, by three: 8 experts, top 2: 64 tokens 6.0, 9.3, 128 7.9, 9.3; 256 experts, top
-// 8: 64 tokens 9.6, 12.4, 128 15.3, 14.0, 256 26.7, 14.2.
+// 8: 64 tokens 9.6, 12.4, 128 15.3, 14.0, 256 26.7, 14.2.  The balanced router, whose workgroup has no more than 64: 64
+// experts, 8 of them: 32 tokens 7.4, 11.9, 64 10.0, 12.7; 256 experts, 8 of 4 of 8 groups: 9.7, 14.4, 14.4, 15.0; of 1,024
+// experts, 4 of them, three launches would be the better from 48 on: 33.9, 38.0, 48 tokens 46.9, 38.0, 64 59.9, 38.7.
 constexpr int kOneLaunch = 64;
 
 // Tokens of a workgroup.  us by 32, by 64: 256 experts, top 8: 16,384 tokens 18.7, 19.6, 32,768 25.9, 24.5, 65,536 38.6, 34.0;
-// 8 experts 13.8, 13.9, 15.7, 15.3, 21.7, 18.4; 1,024 experts, top 4, 32,768 tokens 49, 58.
+// 8 experts 13.8, 13.9, 15.7, 15.3, 21.7, 18.4; 1,024 experts, top 4, 32,768 tokens 49, 58: for those 32,768 are by 32 too.
+// The balanced router's choices and order: 64 experts, 8 of them, 4,096 tokens 17.9, 20.3, 16,384 20.5, 20.6, 32,768 27.3,
+// 25.2, 65,536 43.2, 36.2; 256 experts, 8 of 4 of 8 groups, 18.5, 22.8, 24.2, 25.7, 39.4, 36.6, 61.1, 53.4; 1,024, 4 of
+// them, 45.4, 71.6, 56.1, 78.8, 69.3, 92.6, 138.7, 114.9.
 __host__ __device__ inline int group_tokens(int64_t tokens) { return tokens <= 64 * 512 ? 32 : 64; }
 
 // Neighbouring elements of a lane: those that it loads and stores at once where vectors are aligned; where they are not
