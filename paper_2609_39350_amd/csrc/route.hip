@@ -207,8 +207,8 @@ __global__ __launch_bounds__(kThreads) void k_place(const int32_t *__restrict__ 
 
 // d_logits.  Over all experts d_i = p_i (g_i - sum_j g_j w_j), g 0 for experts not chosen: p again from the logits.
 // Renormalised: w_j (g_j - sum g w) at the chosen, 0 elsewhere, and the logits are not read.
-// BALANCED: weights that were multiplied by a scale (the renormalised form's sum is over it), and where the scores are
-// sigmoids w_j (g_j - the same sum, if renormalised) (1 - s_j) at the chosen.
+// BALANCED: weights that were multiplied by a scale (the renormalised form's sum is of shares w_j / scale), and where the
+// scores are sigmoids w_j (g_j - the same sum, if renormalised) (1 - s_j) at the chosen.
 template <typename T, int PER, bool VEC, bool BALANCED>
 __global__ __launch_bounds__(kThreads) void k_route_backward(
     const T *__restrict__ logits, int64_t stride, int64_t tokens, int experts, int top_k,
@@ -231,10 +231,12 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
         who[h] = j < top_k ? expert[t * top_k + j] : -1;
         w[h] = who[h] >= 0 ? weight[t * top_k + j] : 0.0f;
         g[h] = who[h] >= 0 ? d_weight[t * top_k + j] : 0.0f;
-        gw[h] = g[h] * w[h];
+        // a choice by itself has a share of 1, not of 1 but for a rounding: its gradient is 0
+        const float share = BALANCED && renormalize ? w[h] / scale : w[h];
+        gw[h] = g[h] * share;
     }
     float mean = row_reduce(gw[0] + gw[1], Sum());
-    if constexpr (BALANCED) mean = renormalize ? mean / scale : sigmoid ? 0.0f : mean;
+    if (BALANCED && sigmoid && !renormalize) mean = 0.0f;
     float d[PER];
     if (renormalize || (BALANCED && sigmoid)) {
 #pragma unroll
